@@ -45,7 +45,8 @@
  *   - element types: SCKV_F32 (float) or SCKV_BF16 (bfloat16, stored as
  *     16-bit words); accumulation is always fp32;
  *   - supported head dimensions: 64 and 80;
- *   - device buffers must be 16-byte aligned;
+ *   - device buffers must be 16-byte aligned (accumulated weights w, w_in and
+ *     w_out and the int32 arrays: 4-byte);
  *   - arguments are checked on the host before any HIP call; a failed check
  *     returns SCKV_EINVAL / SCKV_ESPAN / SCKV_EUNSUP and enqueues nothing; a
  *     HIP error returns SCKV_EHIP; sckv_last_error() describes the last
@@ -428,6 +429,162 @@ int kv_start(int32_t* kv_len, int32_t* tok_idx, int32_t* pos_ids, int32_t* cur_t
 int kv_commit(int32_t* kv_len, int32_t* tok_idx, int32_t* pos_ids, int32_t* cur_tok,
               const int32_t* vu, const int32_t* pos, int32_t L_meta, int32_t b, int32_t L_cap,
               int32_t* status, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * RMS norm of each head's queries and keys and the rotation at the tied
+ * positions in one pass, for models that normalise q and k by the head:
+ *   y = x / sqrt(mean(x^2) + eps) * weight, then rope_apply's rotation;
+ *   v is copied.
+ * q, k, v   : (b, H, n, d_head) with element strides x_stride_b, x_stride_h
+ *             and x_stride_row (the same for all three; multiples of 16
+ *             bytes, at least 0, rows of d_head contiguous elements), so that
+ *             a fused projection's token-major output is read as it lies.
+ *             Each is nullable together with its output (q with q_out, ...).
+ * q_out     : (b, H, n, d_head), slice stride q_out_stride_bh; row t of x goes
+ *             to row t.
+ * k_out, v_out : (b, H, kv_rows, d_head), slice stride kv_stride_bh; row t of
+ *             x goes to row row0[s] + t (row0 null: to row t, n <= kv_rows).
+ *             As in rope_apply_at, a sequence with row0 < 0 or
+ *             row0 + n > kv_rows has no key or value written and sets
+ *             SCKV_STATUS_CAP in status.
+ * q_weight, k_weight : [d_head] of type dt, nullable (ones).
+ * eps       : > 0, finite.
+ * pos, L_meta, theta : as for rope_apply; theta == 0 normalises only and pos
+ *             may be null.
+ * cur_tok   : nullable [b], device.  Null: row t is token tok0 + t.  Set: row
+ *             t of sequence s is token cur_tok[s] + t and tok0 is ignored (the
+ *             decode step's form, n = 1: pass q_out and k_out to
+ *             compacted_decode_attn with rope_theta = 0); a row whose token is
+ *             outside [0, L_meta) is written as NaN (v is copied) and sets
+ *             SCKV_STATUS_TOKEN in status.
+ * The norm and the rotation are computed in fp32 (angles in fp64) and rounded
+ * once, at the end.  The squares are summed in fp32, as the inputs stand: a
+ * row whose squares leave its range gives what that sum gives.  An output may
+ * be its input (same address and strides); other overlaps are not allowed.
+ * ------------------------------------------------------------------------- */
+int qk_norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_out,
+                 void* v_out, const void* q_weight, const void* k_weight, float eps, int32_t b,
+                 int32_t H, int32_t n, int64_t x_stride_b, int64_t x_stride_h,
+                 int64_t x_stride_row, int64_t q_out_stride_bh, int64_t kv_stride_bh,
+                 int32_t kv_rows, int32_t d_head, sckv_dtype dt, const int32_t* pos,
+                 int32_t L_meta, int32_t tok0, const int32_t* cur_tok, const int32_t* row0,
+                 float theta, int32_t* status, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Accumulated attention weight of cache rows: what the queries of a prompt
+ * (or of a block of it) give each row,
+ *   w_out[s,h,r] = w_in[s,h,r] + sum_i softmax_r(scale * q_i . k_r),
+ * over the rows that token tok0 + i may see among those the cache holds
+ * (the rule of the span metadata above).  A query that sees none of them adds
+ * nothing.
+ *
+ * q        : (b, H, nq, d_head), slice stride q_stride_bh: tokens tok0 ..
+ *            tok0 + nq - 1 (rotated as the keys are).  nq = 0 adds nothing and
+ *            q may be null.
+ * k_cache  : (b, H, L_cap, d_head) keys, slice stride kv_stride_bh.
+ * w_in     : [b][H][L_cap] float, nullable (zeros); w_out may be w_in.
+ * w_out    : [b][H][L_cap] float; rows [0, kv_len[s]) are written, others are
+ *            left as they are.
+ * kv_len, tok_idx : [b], [b][L_cap]: row r < kv_len[s] holds token
+ *            tok_idx[s][r] (kv_len is clamped to [0, L_cap]; a row whose token
+ *            lies outside [0, L_meta) is seen by none).
+ * ws       : >= sckv_attn_weights_workspace_bytes(b, H, nq, L_cap) bytes
+ *            (overwritten; calls that share one must be ordered).
+ * Limits: nq, L_cap <= 65536.  The sums are fp32 and their order is fixed by
+ * the shapes and the metadata: equal calls give equal bits.
+ * ------------------------------------------------------------------------- */
+size_t sckv_attn_weights_workspace_bytes(int32_t b, int32_t H, int32_t nq, int32_t L_cap);
+int cached_attn_weights(const void* q, const void* k_cache, const float* w_in, float* w_out,
+                        int32_t b, int32_t H, int32_t nq, int32_t d_head, int64_t q_stride_bh,
+                        int64_t kv_stride_bh, sckv_dtype dt, float scale, const int32_t* vu,
+                        int32_t L_meta, int32_t tok0, const int32_t* kv_len,
+                        const int32_t* tok_idx, int32_t L_cap, void* ws, size_t ws_bytes,
+                        hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * compacted_decode_attn that also adds the weight the step gives each row:
+ *   w_out[s,h,r] = w_in[s,h,r] + p_r  for r < kv_len[s],
+ *   w_out[s,h,kv_len[s]] = p of the new row (w_in is not read there),
+ * with p the softmax weights of the output.  Rows behind are left as they
+ * are.  A <CL> step and a failed one add nothing (rows r < kv_len[s], clamped
+ * to [0, L_cap], get w_in; nothing is written for the new row).
+ * w_in, w_out : [b][H][L_cap] float; w_in nullable (zeros); w_out may be w_in.
+ * ws       : >= sckv_decode_weights_workspace_bytes(b, H, L_cap, d_head).
+ * Everything else as for compacted_decode_attn, whose outputs these are.
+ * ------------------------------------------------------------------------- */
+size_t sckv_decode_weights_workspace_bytes(int32_t b, int32_t H, int32_t L_cap, int32_t d_head);
+int compacted_decode_attn_weights(const void* q, const void* k_new, const void* v_new,
+                                  void* k_cache, void* v_cache, const int32_t* kv_len,
+                                  const int32_t* cur_tok, const int32_t* vu, const int32_t* pos,
+                                  int32_t L_meta, void* o, const float* w_in, float* w_out,
+                                  int32_t b, int32_t H, int32_t L_cap, int32_t d_head,
+                                  sckv_dtype dt, float scale, float rope_theta, void* ws,
+                                  size_t ws_bytes, int32_t* status, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Eviction by accumulated weight: each sequence keeps its `recent` last rows
+ * and, of the rows before them, the `heavy` of largest total weight
+ *   total[s][r] = sum over layers m and heads h of w[m][s][h][r]
+ * (summed in fp64, rounded to fp32; equal totals: the lower row stays; a NaN
+ * counts as larger than any number, so a row that holds one stays).  Survivors
+ * keep their order, token index and position id, as in kv_compact.  A
+ * sequence of at most heavy + recent rows is left as it is.
+ *
+ * kv, kv_out : (M, 2, b, H, L_cap, d_head) as for kv_compact (kv_out nullable:
+ *            in place).
+ * w, w_out : (M, b, H, L_cap) float sums, moved as the rows are (w_out
+ *            nullable: in place); those behind the survivors become 0.
+ * heavy, recent : >= 0, heavy + recent >= 1.
+ * kv_len, tok_idx, pos_ids : in/out, as for kv_compact.
+ * total    : [b][L_cap] float out: the totals of rows [0, kv_len[s]) as they
+ *            were before the call; rows behind are left as they are.
+ * kept_src_row : [b][L_cap] out, as for kv_compact.
+ * Limit: L_cap <= 65536.
+ * ------------------------------------------------------------------------- */
+int kv_evict(void* kv, void* kv_out, float* w, float* w_out, int32_t M, int32_t b, int32_t H,
+             int32_t L_cap, int32_t d_head, sckv_dtype dt, int32_t* kv_len, int32_t* tok_idx,
+             int32_t* pos_ids, int32_t heavy, int32_t recent, float* total,
+             int32_t* kept_src_row, hipStream_t stream);
+
+/* Moves accumulated weights as a kv_compact or kv_evict before it moved the
+ * cache's rows: row r of a slice gets the sum of row kept_src_row[s][r] for
+ * r < kv_len[s] (the new length) and 0 behind.  w, w_out: (M, b, H, L_cap);
+ * w_out nullable (in place).  kept_src_row must ascend, as both calls leave
+ * it.  Limit: L_cap <= 65536. */
+int kv_compact_weights(float* w, float* w_out, int32_t M, int32_t b, int32_t H, int32_t L_cap,
+                       const int32_t* kv_len, const int32_t* kept_src_row, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * One decode step of one layer for sequences that continue shared prefixes:
+ * sequence s attends over the rows of prefix s / (b / n_prefix), which is
+ * stored and read once for all of its sequences, and over its own cache
+ * (several samples for one compressed document, Section 4.2; many requests
+ * behind one system prompt).
+ *   o[s,h] = softmax(scale * q . [K_prefix; K_own; k_new]) [V_prefix; V_own; v_new]
+ *
+ * k_prefix, v_prefix : (n_prefix, H, P_cap, d_head) layer slices of the
+ *            prefixes' cache; rows [0, prefix_len[g]) are attended (clamped to
+ *            [0, P_cap]), without a mask: as for compacted_decode_attn they
+ *            hold only tokens that every continuation may see.  Not written.
+ * prefix_len : [n_prefix].   b must be a multiple of n_prefix.
+ * k_cache, v_cache, kv_len : the sequences' own rows, behind their prefix.
+ * cur_tok indexes vu and pos of the whole sequence, prefix included.
+ * ws       : >= sckv_shared_decode_workspace_bytes(b, H, n_prefix, P_cap,
+ *            L_cap, d_head) bytes (overwritten; calls that share one must be
+ *            ordered).
+ * Everything else as for compacted_decode_attn, new row, <CL> steps, failures
+ * and status included.
+ * ------------------------------------------------------------------------- */
+size_t sckv_shared_decode_workspace_bytes(int32_t b, int32_t H, int32_t n_prefix, int32_t P_cap,
+                                          int32_t L_cap, int32_t d_head);
+int shared_prefix_decode_attn(const void* q, const void* k_new, const void* v_new,
+                              const void* k_prefix, const void* v_prefix,
+                              const int32_t* prefix_len, int32_t n_prefix, int32_t P_cap,
+                              void* k_cache, void* v_cache, const int32_t* kv_len,
+                              const int32_t* cur_tok, const int32_t* vu, const int32_t* pos,
+                              int32_t L_meta, void* o, int32_t b, int32_t H, int32_t L_cap,
+                              int32_t d_head, sckv_dtype dt, float scale, float rope_theta,
+                              void* ws, size_t ws_bytes, int32_t* status, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -94,6 +94,21 @@ _SIGS = {
     "local_decode_attn": (ctypes.c_int, [_p, _p, _p, _p, _p, _i32, _p, _p, _p, _i32, _p, _i32,
                                          _i32, _i32, _i32, ctypes.c_int, _f32, _f32, _p, _sz, _p,
                                          _p]),
+    "qk_norm_rope": (ctypes.c_int, [_p] * 8 + [_f32, _i32, _i32, _i32] + [_i64] * 5
+                     + [_i32, _i32, ctypes.c_int, _p, _i32, _i32, _p, _p, _f32, _p, _p]),
+    "sckv_attn_weights_workspace_bytes": (_sz, [_i32] * 4),
+    "cached_attn_weights": (ctypes.c_int, [_p] * 4 + [_i32] * 4
+                            + [_i64, _i64, ctypes.c_int, _f32, _p, _i32, _i32, _p, _p, _i32, _p,
+                               _sz, _p]),
+    "sckv_decode_weights_workspace_bytes": (_sz, [_i32] * 4),
+    "compacted_decode_attn_weights": (ctypes.c_int, [_p] * 9 + [_i32, _p, _p, _p] + [_i32] * 4
+                                      + [ctypes.c_int, _f32, _f32, _p, _sz, _p, _p]),
+    "kv_evict": (ctypes.c_int, [_p] * 4 + [_i32] * 5 + [ctypes.c_int, _p, _p, _p, _i32, _i32, _p,
+                                                        _p, _p]),
+    "kv_compact_weights": (ctypes.c_int, [_p, _p] + [_i32] * 4 + [_p, _p, _p]),
+    "sckv_shared_decode_workspace_bytes": (_sz, [_i32] * 6),
+    "shared_prefix_decode_attn": (ctypes.c_int, [_p] * 6 + [_i32, _i32] + [_p] * 6 + [_i32, _p]
+                                  + [_i32] * 4 + [ctypes.c_int, _f32, _f32, _p, _sz, _p, _p]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(lib, _name)
@@ -163,7 +178,8 @@ def _nat():
             raise ImportError("the native half of the binding (_bind.so) cannot be loaded: build "
                               "it with `python -m paper_2310_08152_amd.build`") from e
         _bind.init({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _SIGS},
-                   _raw_stream)
+                   _raw_stream, getattr(_torch._C, "_cuda_getDevice", None)
+                   or _torch.cuda.current_device)
         _native = _bind
     return _native
 
@@ -575,3 +591,201 @@ def local_decode_attn(q, k_new, v_new, k_cache, v_cache, W: int, cur_tok, vu, po
                                  _dev(cur_tok, "cur_tok", "i32", b, True), pvu, ppos, L_meta, po,
                                  b, H, L_cap, d_head, _dtype_code(q), scale, rope_theta, pw, nw,
                                  pst, _stream(stream, q)))
+
+
+# ---------------------------------------------------------------------------
+# operators beside the compacted cache.  Their tensors must share one device;
+# where it is not the current one, it is made current for the launch.
+# ---------------------------------------------------------------------------
+
+def _device(*tensors):
+    """Context that makes the tensors' device current; they must share one."""
+    torch = _torch or _tm()
+    devs = {t.device for t in tensors if isinstance(t, torch.Tensor)}
+    if len(devs) > 1:
+        _fail("tensors on several devices: " + ", ".join(sorted(map(str, devs))))
+    return torch.cuda.device(devs.pop())
+
+
+def _strided(t, what, b, H, n, d, sb, sh, sr, dtype=None):
+    """(b, H, n, d) rows with strides sb, sh and sr of their own; a tensor of
+    another rank must be contiguous."""
+    if t is not None and t.dim() == 4:
+        if tuple(t.shape) != (b, H, n, d):
+            _fail(f"{what}: shape {tuple(t.shape)}, expected {(b, H, n, d)}")
+        st = t.stride()
+        if st[3] != 1 or any(m > 1 and x != y for m, x, y in zip((b, H, n), st, (sb, sh, sr))):
+            _fail(f"{what}: strides {st}, expected {(sb, sh, sr, 1)}")
+    elif t is not None and not t.is_contiguous():
+        _fail(f"{what}: expected a (b, H, n, d) view or a contiguous tensor")
+    if min(sb, sh, sr) < 0:
+        _fail(f"{what}: negative stride")
+    p = _dev(t, what, "float",
+             (b - 1) * sb + (H - 1) * sh + (n - 1) * sr + d if b and H and n else 0)
+    if dtype is not None and t.dtype != dtype:
+        _fail(f"{what}: element type {t.dtype} differs from {dtype}")
+    return p
+
+
+def _typed(t, what, dtype, need, nullable=False):
+    """A contiguous device array of `dtype` with at least `need` elements."""
+    p = _dev(t, what, None, need, True, nullable)
+    if t is not None and t.dtype != dtype:
+        _fail(f"{what}: must be {dtype}, got {t.dtype}")
+    return p
+
+
+def _sums(t, what, need, nullable=False):
+    """Accumulated weights: a contiguous fp32 device array."""
+    return _typed(t, what, (_torch or _tm()).float32, need, nullable)
+
+
+def qk_norm_rope(q, k, v, q_out, k_out, v_out, q_weight, k_weight, eps: float, b: int, H: int,
+                 n: int, x_stride_b: int, x_stride_h: int, x_stride_row: int,
+                 q_out_stride_bh: int, kv_stride_bh: int, kv_rows: int, d_head: int, pos,
+                 L_meta: int, tok0: int, cur_tok, row0, theta: float, status=None, stream=None):
+    if _done((_native or _nat()).qk_norm_rope(q, k, v, q_out, k_out, v_out, q_weight, k_weight,
+                                              eps, b, H, n, x_stride_b, x_stride_h, x_stride_row,
+                                              q_out_stride_bh, kv_stride_bh, kv_rows, d_head, pos,
+                                              L_meta, tok0, cur_tok, row0, theta, status, stream)):
+        return
+    first = q if q is not None else k if k is not None else v
+    for x, y, nm in ((q, q_out, "q"), (k, k_out, "k"), (v, v_out, "v")):
+        if (x is None) != (y is None):
+            _fail(f"qk_norm_rope: {nm} and {nm}_out go together")
+    if first is None:
+        _fail("qk_norm_rope: one of q, k and v is needed")
+    dt = first.dtype
+    args = [None if x is None else _strided(x, nm, b, H, n, d_head, x_stride_b, x_stride_h,
+                                            x_stride_row, dt)
+            for x, nm in ((q, "q"), (k, "k"), (v, "v"))]
+    args.append(None if q is None else _rows(q_out, "q_out", b, H, n, d_head, q_out_stride_bh, dt))
+    for x, y, nm in ((k, k_out, "k_out"), (v, v_out, "v_out")):
+        args.append(None if x is None else _rows(y, nm, b, H, kv_rows, d_head, kv_stride_bh, dt))
+    args += [_typed(q_weight, "q_weight", dt, d_head, True),
+             _typed(k_weight, "k_weight", dt, d_head, True)]
+    tail = [_dev(pos, "pos", "i32", b * L_meta, True, nullable=theta == 0), L_meta, tok0,
+            _dev(cur_tok, "cur_tok", "i32", b, True, nullable=True),
+            _dev(row0, "row0", "i32", b, True, nullable=True), theta,
+            _dev(status, "status", "i32", 1, nullable=True)]
+    with _device(q, k, v, q_out, k_out, v_out, q_weight, k_weight, pos, cur_tok, row0, status):
+        _check(lib.qk_norm_rope(*args, eps, b, H, n, x_stride_b, x_stride_h, x_stride_row,
+                                q_out_stride_bh, kv_stride_bh, kv_rows, d_head,
+                                _dtype_code(first), *tail, _stream(stream, first)))
+
+
+def sckv_attn_weights_workspace_bytes(b: int, H: int, nq: int, L_cap: int) -> int:
+    return int(lib.sckv_attn_weights_workspace_bytes(b, H, nq, L_cap))
+
+
+def cached_attn_weights(q, k_cache, w_in, w_out, b: int, H: int, nq: int, d_head: int,
+                        q_stride_bh: int, kv_stride_bh: int, scale: float, vu, L_meta: int,
+                        tok0: int, kv_len, tok_idx, L_cap: int, ws, stream=None):
+    if _done((_native or _nat()).cached_attn_weights(q, k_cache, w_in, w_out, b, H, nq, d_head,
+                                                     q_stride_bh, kv_stride_bh, scale, vu, L_meta,
+                                                     tok0, kv_len, tok_idx, L_cap, ws, stream)):
+        return
+    pq = _rows(q, "q", b, H, nq, d_head, q_stride_bh)
+    pk = _rows(k_cache, "k_cache", b, H, L_cap, d_head, kv_stride_bh, q.dtype)
+    pwi = _sums(w_in, "w_in", b * H * L_cap, True)
+    pwo = _sums(w_out, "w_out", b * H * L_cap)
+    pvu = _dev(vu, "vu", "i32", b * L_meta, True)
+    pl = _dev(kv_len, "kv_len", "i32", b, True)
+    pt = _dev(tok_idx, "tok_idx", "i32", b * L_cap, True)
+    pw, nw = _ws(ws)
+    with _device(q, k_cache, w_in, w_out, vu, kv_len, tok_idx, ws):
+        _check(lib.cached_attn_weights(pq, pk, pwi, pwo, b, H, nq, d_head, q_stride_bh,
+                                       kv_stride_bh, _dtype_code(q), scale, pvu, L_meta, tok0, pl,
+                                       pt, L_cap, pw, nw, _stream(stream, q)))
+
+
+def sckv_decode_weights_workspace_bytes(b: int, H: int, L_cap: int, d_head: int) -> int:
+    return int(lib.sckv_decode_weights_workspace_bytes(b, H, L_cap, d_head))
+
+
+def compacted_decode_attn_weights(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos,
+                                  L_meta: int, o, w_in, w_out, b: int, H: int, L_cap: int,
+                                  d_head: int, scale: float, rope_theta: float, ws, status=None,
+                                  stream=None):
+    if _done((_native or _nat()).compacted_decode_attn_weights(
+            q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos, L_meta, o, w_in, w_out, b,
+            H, L_cap, d_head, scale, rope_theta, ws, status, stream)):
+        return
+    pq, pkn, pvn, pkc, pvc, po, pvu, ppos, pst = _decode_args(
+        q, k_new, v_new, k_cache, v_cache, o, vu, pos, L_meta, b, H, L_cap, d_head, rope_theta,
+        status)
+    pl, pc = (_dev(t, nm, "i32", b, True) for t, nm in ((kv_len, "kv_len"), (cur_tok, "cur_tok")))
+    pwi = _sums(w_in, "w_in", b * H * L_cap, True)
+    pwo = _sums(w_out, "w_out", b * H * L_cap)
+    pw, nw = _ws(ws)
+    with _device(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos, o, w_in, w_out, ws,
+                 status):
+        _check(lib.compacted_decode_attn_weights(pq, pkn, pvn, pkc, pvc, pl, pc, pvu, ppos, L_meta,
+                                                 po, pwi, pwo, b, H, L_cap, d_head,
+                                                 _dtype_code(q), scale, rope_theta, pw, nw, pst,
+                                                 _stream(stream, q)))
+
+
+def kv_evict(kv, kv_out, w, w_out, M: int, b: int, H: int, L_cap: int, d_head: int, kv_len,
+             tok_idx, pos_ids, heavy: int, recent: int, total, kept_src_row, stream=None):
+    if _done((_native or _nat()).kv_evict(kv, kv_out, w, w_out, M, b, H, L_cap, d_head, kv_len,
+                                          tok_idx, pos_ids, heavy, recent, total, kept_src_row,
+                                          stream)):
+        return
+    n = M * 2 * b * H * L_cap * d_head
+    pkv = _dev(kv, "kv", "float", n, True)
+    pout = _typed(kv_out, "kv_out", kv.dtype, n, True)
+    pw = _sums(w, "w", M * b * H * L_cap)
+    pwo = _sums(w_out, "w_out", M * b * H * L_cap, True)
+    args = (_dev(kv_len, "kv_len", "i32", b, True),
+            _dev(tok_idx, "tok_idx", "i32", b * L_cap, True),
+            _dev(pos_ids, "pos_ids", "i32", b * L_cap, True), heavy, recent,
+            _sums(total, "total", b * L_cap),
+            _dev(kept_src_row, "kept_src_row", "i32", b * L_cap, True))
+    with _device(kv, kv_out, w, w_out, kv_len, tok_idx, pos_ids, total, kept_src_row):
+        _check(lib.kv_evict(pkv, pout, pw, pwo, M, b, H, L_cap, d_head, _dtype_code(kv), *args,
+                            _stream(stream, kv)))
+
+
+def kv_compact_weights(w, w_out, M: int, b: int, H: int, L_cap: int, kv_len, kept_src_row,
+                       stream=None):
+    if _done((_native or _nat()).kv_compact_weights(w, w_out, M, b, H, L_cap, kv_len, kept_src_row,
+                                                    stream)):
+        return
+    pw = _sums(w, "w", M * b * H * L_cap)
+    pwo = _sums(w_out, "w_out", M * b * H * L_cap, True)
+    pl = _dev(kv_len, "kv_len", "i32", b, True)
+    ps = _dev(kept_src_row, "kept_src_row", "i32", b * L_cap, True)
+    with _device(w, w_out, kv_len, kept_src_row):
+        _check(lib.kv_compact_weights(pw, pwo, M, b, H, L_cap, pl, ps, _stream(stream, w)))
+
+
+def sckv_shared_decode_workspace_bytes(b: int, H: int, n_prefix: int, P_cap: int, L_cap: int,
+                                       d_head: int) -> int:
+    return int(lib.sckv_shared_decode_workspace_bytes(b, H, n_prefix, P_cap, L_cap, d_head))
+
+
+def shared_prefix_decode_attn(q, k_new, v_new, k_prefix, v_prefix, prefix_len, n_prefix: int,
+                              P_cap: int, k_cache, v_cache, kv_len, cur_tok, vu, pos, L_meta: int,
+                              o, b: int, H: int, L_cap: int, d_head: int, scale: float,
+                              rope_theta: float, ws, status=None, stream=None):
+    if _done((_native or _nat()).shared_prefix_decode_attn(
+            q, k_new, v_new, k_prefix, v_prefix, prefix_len, n_prefix, P_cap, k_cache, v_cache,
+            kv_len, cur_tok, vu, pos, L_meta, o, b, H, L_cap, d_head, scale, rope_theta, ws,
+            status, stream)):
+        return
+    pq, pkn, pvn, pkc, pvc, po, pvu, ppos, pst = _decode_args(
+        q, k_new, v_new, k_cache, v_cache, o, vu, pos, L_meta, b, H, L_cap, d_head, rope_theta,
+        status)
+    np_ = n_prefix * H * P_cap * d_head
+    pkp, pvp = (_typed(t, nm, q.dtype, np_) for t, nm in ((k_prefix, "k_prefix"),
+                                                          (v_prefix, "v_prefix")))
+    ppl = _dev(prefix_len, "prefix_len", "i32", n_prefix, True)
+    pl, pc = (_dev(t, nm, "i32", b, True) for t, nm in ((kv_len, "kv_len"), (cur_tok, "cur_tok")))
+    pw, nw = _ws(ws)
+    with _device(q, k_new, v_new, k_prefix, v_prefix, prefix_len, k_cache, v_cache, kv_len, cur_tok,
+                 vu, pos, o, ws, status):
+        _check(lib.shared_prefix_decode_attn(pq, pkn, pvn, pkp, pvp, ppl, n_prefix, P_cap, pkc,
+                                             pvc, pl, pc, pvu, ppos, L_meta, po, b, H, L_cap,
+                                             d_head, _dtype_code(q), scale, rope_theta, pw, nw,
+                                             pst, _stream(stream, q)))

@@ -21,6 +21,7 @@
 namespace {
 
 PyObject* g_raw_stream = nullptr;  // device index -> the current stream's handle
+PyObject* g_device = nullptr;      // -> the current device's index
 
 #define ENTRY(name) decltype(&::name) p_##name = nullptr;
 #define ENTRIES(X)                                                                               \
@@ -28,7 +29,9 @@ PyObject* g_raw_stream = nullptr;  // device index -> the current stream's handl
   X(kv_extend) X(kv_start) X(kv_compact) X(rope_apply) X(rope_apply_at) X(rope_block)            \
   X(span_masked_prefill_attn)                                                                    \
   X(span_masked_prefill_attn_planned) X(span_masked_prefill_attn_cached)                         \
-  X(span_masked_prefill_attn_cached_planned) X(sckv_prefill_plan) X(sckv_prefill_cached_plan)
+  X(span_masked_prefill_attn_cached_planned) X(sckv_prefill_plan) X(sckv_prefill_cached_plan)    \
+  X(qk_norm_rope) X(cached_attn_weights) X(compacted_decode_attn_weights) X(kv_evict)            \
+  X(kv_compact_weights) X(shared_prefix_decode_attn)
 ENTRIES(ENTRY)
 #undef ENTRY
 
@@ -70,7 +73,18 @@ class Args {
     if (!THPVariable_CheckExact(o)) throw Defer();
     const at::Tensor& t = THPVariable_Unpack(o);
     if (!t.is_cuda() || !t.has_storage()) throw Defer();
+    const int dev = t.get_device();
+    mixed_ = mixed_ || (dev_ >= 0 && dev_ != dev);
+    dev_ = dev;
     return &t;
+  }
+  // every tensor taken so far is on the current device, where a launch goes
+  void on_current_device() const {
+    PyObject* r = PyObject_CallNoArgs(g_device);
+    if (!r) throw Defer();
+    const long dev = PyLong_AsLong(r);
+    Py_DECREF(r);
+    if (mixed_ || dev != dev_) throw Defer();
   }
   // the stream argument, or the current stream of t's device
   hipStream_t stream(const at::Tensor* t) {
@@ -94,6 +108,8 @@ class Args {
  private:
   PyObject* const* a_;
   Py_ssize_t at_ = 0;
+  int dev_ = -1;
+  bool mixed_ = false;
 };
 
 int64_t available(const at::Tensor& t) {
@@ -420,6 +436,190 @@ PyObject* cached_plan(PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (b, H, n, d) rows with strides of their own (see _strided of binding.py)
+void* strided(const at::Tensor* t, int64_t b, int64_t H, int64_t n, int64_t d, int64_t sb,
+              int64_t sh, int64_t sr, sckv_dtype like) {
+  if (type_code(*t) != like || b < 0 || H < 0 || n < 0 || d < 0 || sb < 0 || sh < 0 || sr < 0)
+    throw Defer();
+  if (t->dim() == 4) {
+    if (t->size(0) != b || t->size(1) != H || t->size(2) != n || t->size(3) != d) throw Defer();
+    if ((b > 1 && t->stride(0) != sb) || (H > 1 && t->stride(1) != sh) ||
+        (n > 1 && t->stride(2) != sr) || t->stride(3) != 1)
+      throw Defer();
+  } else if (!t->is_contiguous()) {
+    throw Defer();
+  }
+  if (b > 0 && H > 0 && n > 0 &&
+      (b - 1) * (__int128)sb + (H - 1) * (__int128)sh + (n - 1) * (__int128)sr + d > available(*t))
+    throw Defer();
+  return address(*t);
+}
+
+// an array of 32-bit floats
+float* sums(const at::Tensor* t, int64_t need, bool nullable = false) {
+  if (!t && nullable) return nullptr;
+  return (float*)floats(t, need, SCKV_F32);
+}
+
+PyObject* norm_rope(PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 27);
+  const at::Tensor* x[3] = {g.tensor(), g.tensor(), g.tensor()};
+  const at::Tensor *qo = g.tensor(), *ko = g.tensor(), *vo = g.tensor(), *qw = g.tensor(),
+                   *kw = g.tensor();
+  const float eps = g.f32();
+  const int32_t b = g.i32(), H = g.i32(), rows_ = g.i32();
+  const int64_t xb = g.i64(), xh = g.i64(), xr = g.i64(), qs = g.i64(), ks = g.i64();
+  const int32_t kv_rows = g.i32(), d = g.i32();
+  const at::Tensor* pos = g.tensor();
+  const int32_t L_meta = g.i32(), tok0 = g.i32();
+  const at::Tensor *cur = g.tensor(), *row0 = g.tensor();
+  const double theta_in = g.f64();
+  const at::Tensor* st = g.tensor();
+  const at::Tensor* first = x[0] ? x[0] : x[1] ? x[1] : x[2];
+  if (!first || !x[0] != !qo || !x[1] != !ko || !x[2] != !vo) throw Defer();
+  const sckv_dtype dt = type_code(*first);
+  void* in[3];
+  for (int i = 0; i < 3; ++i) in[i] = x[i] ? strided(x[i], b, H, rows_, d, xb, xh, xr, dt) : nullptr;
+  void *pqo = qo ? rows(qo, b, H, rows_, d, qs, dt) : nullptr,
+       *pko = ko ? rows(ko, b, H, kv_rows, d, ks, dt) : nullptr,
+       *pvo = vo ? rows(vo, b, H, kv_rows, d, ks, dt) : nullptr,
+       *pqw = qw ? floats(qw, d, dt) : nullptr, *pkw = kw ? floats(kw, d, dt) : nullptr;
+  const int32_t *ppos = ints(pos, times({b, L_meta}), theta_in == 0.0), *pcur = ints(cur, b, true),
+                *prow = ints(row0, b, true);
+  int32_t* pst = word(st);
+  g.on_current_device();
+  const hipStream_t stream = g.stream(first);
+  return status_of([&] {
+    return p_qk_norm_rope(in[0], in[1], in[2], pqo, pko, pvo, pqw, pkw, eps, b, H, rows_, xb, xh,
+                          xr, qs, ks, kv_rows, d, dt, ppos, L_meta, tok0, pcur, prow,
+                          (float)theta_in, pst, stream);
+  });
+}
+
+PyObject* attn_weights(PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 19);
+  const at::Tensor *q = g.tensor(), *kc = g.tensor(), *wi = g.tensor(), *wo = g.tensor();
+  const int32_t b = g.i32(), H = g.i32(), nq = g.i32(), d = g.i32();
+  const int64_t qs = g.i64(), ks = g.i64();
+  const float scale = g.f32();
+  const at::Tensor* vu = g.tensor();
+  const int32_t L_meta = g.i32(), tok0 = g.i32();
+  const at::Tensor *len = g.tensor(), *tok = g.tensor();
+  const int32_t L_cap = g.i32();
+  const at::Tensor* ws = g.tensor();
+  if (!q) throw Defer();
+  const sckv_dtype dt = type_code(*q);
+  const int64_t nw = times({b, H, L_cap});
+  void *pq = rows(q, b, H, nq, d, qs, dt), *pk = rows(kc, b, H, L_cap, d, ks, dt);
+  float *pwi = sums(wi, nw, true), *pwo = sums(wo, nw);
+  const int32_t *pvu = ints(vu, times({b, L_meta})), *plen = ints(len, b),
+                *ptok = ints(tok, times({b, L_cap}));
+  const Work w = workspace(ws);
+  g.on_current_device();
+  const hipStream_t stream = g.stream(q);
+  return status_of([&] {
+    return p_cached_attn_weights(pq, pk, pwi, pwo, b, H, nq, d, qs, ks, dt, scale, pvu, L_meta,
+                                 tok0, plen, ptok, L_cap, w.p, w.n, stream);
+  });
+}
+
+// a decode step that also adds weights, or over a shared prefix
+template <bool SHARED>
+PyObject* step(PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, SHARED ? 25 : 22);
+  const at::Tensor *q = g.tensor(), *kn = g.tensor(), *vn = g.tensor();
+  const at::Tensor *kp = nullptr, *vp = nullptr, *plen = nullptr;
+  int32_t G = 0, P_cap = 0;
+  if (SHARED) {
+    kp = g.tensor();
+    vp = g.tensor();
+    plen = g.tensor();
+    G = g.i32();
+    P_cap = g.i32();
+  }
+  const at::Tensor *kc = g.tensor(), *vc = g.tensor(), *len = g.tensor(), *cur = g.tensor(),
+                   *vu = g.tensor(), *pos = g.tensor();
+  const int32_t L_meta = g.i32();
+  const at::Tensor* o = g.tensor();
+  const at::Tensor *wi = nullptr, *wo = nullptr;
+  if (!SHARED) {
+    wi = g.tensor();
+    wo = g.tensor();
+  }
+  const int32_t b = g.i32(), H = g.i32(), L_cap = g.i32(), d = g.i32();
+  const float scale = g.f32();
+  const double theta_in = g.f64();
+  const at::Tensor *ws = g.tensor(), *st = g.tensor();
+  if (!q) throw Defer();
+  const sckv_dtype dt = type_code(*q);
+  const int64_t nh = times({b, H, d}), nc = times({b, H, L_cap, d}), nm = times({b, L_meta});
+  void *pq = floats(q, nh, dt), *pkn = floats(kn, nh, dt), *pvn = floats(vn, nh, dt),
+       *pkc = floats(kc, nc, dt), *pvc = floats(vc, nc, dt), *po = floats(o, nh, dt);
+  const int32_t *pvu = ints(vu, nm), *ppos = ints(pos, nm, theta_in == 0.0), *pcur = ints(cur, b),
+                *pl = ints(len, b);
+  int32_t* pst = word(st);
+  const Work w = workspace(ws);
+  const float theta = (float)theta_in;
+  if (SHARED) {
+    const int64_t np = times({G, H, P_cap, d});
+    const void *pkp = floats(kp, np, dt), *pvp = floats(vp, np, dt);
+    const int32_t* ppl = ints(plen, G);
+    g.on_current_device();
+    const hipStream_t stream = g.stream(q);
+    return status_of([&] {
+      return p_shared_prefix_decode_attn(pq, pkn, pvn, pkp, pvp, ppl, G, P_cap, pkc, pvc, pl, pcur,
+                                         pvu, ppos, L_meta, po, b, H, L_cap, d, dt, scale, theta,
+                                         w.p, w.n, pst, stream);
+    });
+  }
+  const int64_t nw = times({b, H, L_cap});
+  float *pwi = sums(wi, nw, true), *pwo = sums(wo, nw);
+  g.on_current_device();
+  const hipStream_t stream = g.stream(q);
+  return status_of([&] {
+    return p_compacted_decode_attn_weights(pq, pkn, pvn, pkc, pvc, pl, pcur, pvu, ppos, L_meta, po,
+                                           pwi, pwo, b, H, L_cap, d, dt, scale, theta, w.p, w.n,
+                                           pst, stream);
+  });
+}
+
+PyObject* evict(PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 17);
+  const at::Tensor *kv = g.tensor(), *out = g.tensor(), *w = g.tensor(), *wo = g.tensor();
+  const int32_t M = g.i32(), b = g.i32(), H = g.i32(), L_cap = g.i32(), d = g.i32();
+  const at::Tensor *len = g.tensor(), *tok = g.tensor(), *ids = g.tensor();
+  const int32_t heavy = g.i32(), recent = g.i32();
+  const at::Tensor *total = g.tensor(), *src = g.tensor();
+  if (!kv) throw Defer();
+  const sckv_dtype dt = type_code(*kv);
+  const int64_t all = times({M, 2, b, H, L_cap, d}), nw = times({M, b, H, L_cap}),
+                nc = times({b, L_cap});
+  void *pkv = floats(kv, all, dt), *pout = out ? floats(out, all, dt) : nullptr;
+  float *pw = sums(w, nw), *pwo = sums(wo, nw, true), *ptot = sums(total, nc);
+  int32_t *plen = ints(len, b), *ptok = ints(tok, nc), *pids = ints(ids, nc), *psrc = ints(src, nc);
+  g.on_current_device();
+  const hipStream_t stream = g.stream(kv);
+  return status_of([&] {
+    return p_kv_evict(pkv, pout, pw, pwo, M, b, H, L_cap, d, dt, plen, ptok, pids, heavy, recent,
+                      ptot, psrc, stream);
+  });
+}
+
+PyObject* compact_weights(PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 9);
+  const at::Tensor *w = g.tensor(), *wo = g.tensor();
+  const int32_t M = g.i32(), b = g.i32(), H = g.i32(), L_cap = g.i32();
+  const at::Tensor *len = g.tensor(), *src = g.tensor();
+  const int64_t nw = times({M, b, H, L_cap});
+  float *pw = sums(w, nw), *pwo = sums(wo, nw, true);
+  const int32_t *plen = ints(len, b), *psrc = ints(src, times({b, L_cap}));
+  g.on_current_device();
+  const hipStream_t stream = g.stream(w);
+  return status_of([&] {
+    return p_kv_compact_weights(pw, pwo, M, b, H, L_cap, plen, psrc, stream);
+  });
+}
+
 // no C++ exception crosses into Python: whatever a check throws, binding.py
 // takes over
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
@@ -432,10 +632,10 @@ PyObject* guarded(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
-// init({entry name: address}, stream query)
+// init({entry name: address}, stream query, device query)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 2 || !PyDict_Check(a[0])) {
-    PyErr_SetString(PyExc_TypeError, "init(dict of entry points, stream query)");
+  if (n != 3 || !PyDict_Check(a[0])) {
+    PyErr_SetString(PyExc_TypeError, "init(dict of entry points, stream query, device query)");
     return nullptr;
   }
 #define TAKE(name)                                                    \
@@ -452,6 +652,8 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #undef TAKE
   Py_INCREF(a[1]);
   Py_XSETREF(g_raw_stream, a[1]);
+  Py_INCREF(a[2]);
+  Py_XSETREF(g_device, a[2]);
   Py_RETURN_NONE;
 }
 
@@ -474,6 +676,12 @@ PyMethodDef methods[] = {
     METHOD("span_masked_prefill_attn_cached_planned", cached<true>),
     METHOD("sckv_prefill_plan", plan),
     METHOD("sckv_prefill_cached_plan", cached_plan),
+    METHOD("qk_norm_rope", norm_rope),
+    METHOD("cached_attn_weights", attn_weights),
+    METHOD("compacted_decode_attn_weights", step<false>),
+    METHOD("shared_prefix_decode_attn", step<true>),
+    METHOD("kv_evict", evict),
+    METHOD("kv_compact_weights", compact_weights),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods,

@@ -183,6 +183,23 @@ __global__ __launch_bounds__(MOVE_THREADS) void compact_move_kernel(
   }
 }
 
+int launch_move(void* kv, void* kv_out, int32_t M, int32_t b, int32_t H, int32_t L_cap,
+                int32_t d_head, sckv_dtype dt, const int32_t* kv_len, const int32_t* kept_src,
+                const char* what, hipStream_t stream) {
+  const int rowb = d_head * elem_bytes(dt);
+  char* a = static_cast<char*>(kv);
+  char* o = static_cast<char*>(kv_out);
+  const unsigned g = (unsigned)((int64_t)M * 2 * b * H);
+  switch (rowb) {
+    case 128: compact_move_kernel<128, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src); break;
+    case 160: compact_move_kernel<160, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src); break;
+    case 256: compact_move_kernel<256, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src); break;
+    case 320: compact_move_kernel<320, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src); break;
+    default: return fail(SCKV_EUNSUP, std::string(what) + ": unsupported row size");
+  }
+  return hip_check(hipGetLastError(), what);
+}
+
 }  // namespace sckv
 
 using namespace sckv;
@@ -211,16 +228,6 @@ extern "C" int kv_compact(void* kv, void* kv_out, int32_t M, int32_t b, int32_t 
                                                      L_cap, kept_src_row);
   int rc = hip_check(hipGetLastError(), "kv_compact: scan launch");
   if (rc) return rc;
-  const int rowb = d_head * elem_bytes(dt);
-  char* a = static_cast<char*>(kv);
-  char* o = static_cast<char*>(kv_out);
-  const unsigned g = (unsigned)slices;
-  switch (rowb) {
-    case 128: compact_move_kernel<128, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src_row); break;
-    case 160: compact_move_kernel<160, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src_row); break;
-    case 256: compact_move_kernel<256, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src_row); break;
-    case 320: compact_move_kernel<320, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src_row); break;
-    default: return fail(SCKV_EUNSUP, "kv_compact: unsupported row size");
-  }
-  return hip_check(hipGetLastError(), "kv_compact: move launch");
+  return launch_move(kv, kv_out, M, b, H, L_cap, d_head, dt, kv_len, kept_src_row,
+                     "kv_compact: move launch", stream);
 }

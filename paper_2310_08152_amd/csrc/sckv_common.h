@@ -20,7 +20,14 @@ void clear_error();
 int fail(int code, const std::string& msg);
 int hip_check(hipError_t e, const char* what);
 
+// moves the rows that kept_src lists to the front of every cache slice
+// (compact.hip); kv_out null: in place
+int launch_move(void* kv, void* kv_out, int32_t M, int32_t b, int32_t H, int32_t L_cap,
+                int32_t d_head, sckv_dtype dt, const int32_t* kv_len, const int32_t* kept_src,
+                const char* what, hipStream_t stream);
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline int elem_bytes(sckv_dtype dt) { return dt == SCKV_F32 ? 4 : 2; }
 inline bool valid_dtype(int dt) { return dt == SCKV_F32 || dt == SCKV_BF16; }
 inline bool supported_d(int d) { return d == 64 || d == 80; }

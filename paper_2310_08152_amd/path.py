@@ -13,6 +13,16 @@ Typical use (one batch of sequences):
 A prompt too long for the cache is processed block by block instead
 (prefill_progressive): each block is appended to the compacted cache,
 attends to it, and the spans it closes are freed before the next block.
+
+Beside that path:
+  * models that normalise q and k by the head: a QKNorm, norm_rope_rows in the
+    place of rope_rows for a prompt, norm= of prefill_progressive and
+    decode_layer;
+  * eviction by accumulated attention weight: cache.track_weights(), then
+    prompt_weights / decode_weights_layer add to cache.w, and
+    cache.evict(heavy, recent) keeps the rows that drew most of it;
+  * sequences that continue a shared prefix: the prefix in a KVCache of its
+    own, cache.start_behind(L) and shared_decode_layer.
 """
 from __future__ import annotations
 
@@ -40,11 +50,19 @@ class SpanMeta:
 
 
 class KVCache:
-    """(M, 2, b, H, L_cap, d) cache with per-sequence row bookkeeping."""
+    """(M, 2, b, H, L_cap, d) cache with per-sequence row bookkeeping (kv: an
+    existing contiguous tensor of that shape to hold the rows)."""
 
-    def __init__(self, M: int, b: int, H: int, L_cap: int, d: int, dtype, device):
+    def __init__(self, M: int, b: int, H: int, L_cap: int, d: int, dtype, device, kv=None):
         self.M, self.b, self.H, self.L_cap, self.d = M, b, H, L_cap, d
-        self.kv = torch.empty(M, 2, b, H, L_cap, d, dtype=dtype, device=device)
+        if kv is None:
+            kv = torch.empty(M, 2, b, H, L_cap, d, dtype=dtype, device=device)
+        elif tuple(kv.shape) != (M, 2, b, H, L_cap, d) or kv.dtype != dtype \
+                or not kv.is_contiguous():
+            raise ValueError(f"kv must be a contiguous {dtype} tensor of shape "
+                             f"{(M, 2, b, H, L_cap, d)}")
+        self.kv = kv
+        self.w = self.total = None  # accumulated weights (track_weights)
         self.kv_len = torch.zeros(b, dtype=torch.int32, device=device)
         self.tok_idx = torch.zeros(b, L_cap, dtype=torch.int32, device=device)
         self.pos_ids = torch.zeros(b, L_cap, dtype=torch.int32, device=device)
@@ -55,6 +73,19 @@ class KVCache:
         # host time, and decode issues one call per layer per token
         self._k = [self.kv[m, 0] for m in range(M)]
         self._v = [self.kv[m, 1] for m in range(M)]
+
+    def track_weights(self, w=None):
+        """Accumulated attention weights beside the rows: w (M, b, H, L_cap)
+        fp32, zeros unless given.  They then follow the rows through compact
+        and evict; another prompt in the same cache starts with w.zero_()."""
+        shape = (self.M, self.b, self.H, self.L_cap)
+        if w is None:
+            w = torch.zeros(shape, dtype=torch.float32, device=self.kv.device)
+        elif tuple(w.shape) != shape or w.dtype != torch.float32 or not w.is_contiguous():
+            raise ValueError(f"w must be a contiguous float32 tensor of shape {shape}")
+        self.w = w
+        self._w = [w[m] for m in range(self.M)]
+        self.total = torch.zeros(self.b, self.L_cap, dtype=torch.float32, device=self.kv.device)
 
     def k(self, m: int):
         return self._k[m]
@@ -85,6 +116,25 @@ class KVCache:
         B.kv_compact(self.kv, kv_out, self.M, self.b, self.H, self.L_cap, self.d, self.kv_len,
                      self.tok_idx, self.pos_ids, nt, meta.vu, meta.L_meta, self.kept_src,
                      stream=stream)
+        if self.w is not None:
+            B.kv_compact_weights(self.w, None, self.M, self.b, self.H, self.L_cap, self.kv_len,
+                                 self.kept_src, stream=stream)
+
+    def evict(self, heavy: int, recent: int, kv_out=None, w_out=None, stream=None):
+        """Keep each sequence's `recent` last rows and, of those before them,
+        the `heavy` with the largest accumulated weight (track_weights).  The
+        totals that decided are left in self.total, at the old rows."""
+        if self.w is None:
+            raise ValueError("evict needs accumulated weights: call track_weights first")
+        B.kv_evict(self.kv, kv_out, self.w, w_out, self.M, self.b, self.H, self.L_cap, self.d,
+                   self.kv_len, self.tok_idx, self.pos_ids, heavy, recent, self.total,
+                   self.kept_src, stream=stream)
+
+    def start_behind(self, L: int):
+        """No rows yet; every sequence's next token is L, the first behind a
+        shared prefix of L tokens (which lies in a cache of its own)."""
+        self.kv_len.zero_()
+        self.cur_tok.fill_(L)
 
     def extend(self, meta: SpanMeta, tok0: int, n: int, row0, stream=None):
         """Rows for prompt tokens tok0 .. tok0+n-1 after the current rows;
@@ -102,9 +152,13 @@ DECODE_PARTIALS = 512  # chunk partials a decode workspace holds at least
 
 class Workspace:
     """Device workspaces sized for a batch shape (block: the block size of
-    block-wise prompt processing, if used)."""
+    block-wise prompt processing, if used; weights: the most queries of one
+    prompt_weights call, at least 1 for decode_weights_layer, if used;
+    prefixes, prefix_rows: the shared prefixes and their row capacity, if
+    used)."""
 
-    def __init__(self, b: int, H: int, L: int, L_cap: int, d: int, device, block: int = 0):
+    def __init__(self, b: int, H: int, L: int, L_cap: int, d: int, device, block: int = 0,
+                 weights: int = 0, prefixes: int = 0, prefix_rows: int = 0):
         self.prefill = torch.empty(max(1, B.sckv_prefill_workspace_bytes(b, max(L, 1))),
                                    dtype=torch.uint8, device=device)
         # room for as many partials as a launch of few slices splits into (512
@@ -117,6 +171,17 @@ class Workspace:
         if block > 0:
             self.prefill_cached = torch.empty(
                 max(1, B.sckv_prefill_cached_workspace_bytes(b, block, L_cap)),
+                dtype=torch.uint8, device=device)
+        self.weights = self.shared = None
+        if weights > 0:
+            self.weights = torch.empty(
+                max(B.sckv_attn_weights_workspace_bytes(b, H, weights, L_cap),
+                    B.sckv_decode_weights_workspace_bytes(b, H, L_cap, d)),
+                dtype=torch.uint8, device=device)
+        if prefixes > 0:
+            self.shared = torch.empty(
+                max(1, B.sckv_shared_decode_workspace_bytes(b, H, prefixes, prefix_rows, L_cap,
+                                                            d)),
                 dtype=torch.uint8, device=device)
 
 
@@ -148,13 +213,120 @@ def prefill_plan(meta: SpanMeta, ws: Workspace, b: int, L: int, stream=None):
     B.sckv_prefill_plan(meta.vu, meta.L_meta, b, L, ws.prefill, stream=stream)
 
 
+class QKNorm:
+    """RMS norm of each head's queries and keys: weights [d] of the cache's
+    type (None: ones) and eps.  The normalised q and k of a decode step go to
+    buffers kept here, made at the first step of a shape; steps that share
+    this object must be ordered, as with a workspace."""
+
+    def __init__(self, q_weight, k_weight, eps: float = 1e-6):
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, eps
+        self._step = None
+
+    def step_buffers(self, q):
+        s = self._step
+        if s is None or s[0].shape != q.shape or s[0].dtype != q.dtype or s[0].device != q.device:
+            s = self._step = tuple(torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                                   for _ in range(2))
+        return s
+
+
+def norm_rope_rows(q, k, v, qr, k_out, v_out, norm: QKNorm, meta: SpanMeta, n: int, tok0: int,
+                   theta: float, row0=None, status=None, stream=None):
+    """Normalise and rotate rows [0, n) of q and k (tokens tok0..) into qr and
+    k_out, and copy v into v_out; k_out and v_out are cache slices, written
+    from row row0[s] on (row 0 without row0).  q, k, v: (b, H, n, d) views of
+    any strides, for instance of a projection's token-major output; those of
+    one stride pattern share a launch."""
+    b, H, _, d = q.shape
+    x = q.stride()
+    sets = ([(q, k, v, qr, k_out, v_out)] if k.stride() == x and v.stride() == x else
+            [(q, None, None, qr, None, None), (None, k, None, None, k_out, None),
+             (None, None, v, None, None, v_out)])
+    for xs in sets:
+        x = next(t for t in xs[:3] if t is not None).stride()
+        B.qk_norm_rope(*xs, norm.q_weight, norm.k_weight, norm.eps, b, H, n, x[0], x[1], x[2],
+                       qr.stride(1), k_out.stride(1), k_out.shape[2], d, meta.pos, meta.L_meta,
+                       tok0, None, row0, theta, status=status, stream=stream)
+
+
+def norm_rope_step(q, k, q_out, k_out, norm: QKNorm, cache: KVCache, meta: SpanMeta,
+                   theta: float, stream=None):
+    """Normalise and rotate one token's q and k (b, H, d) a sequence, at the
+    cache's current tokens."""
+    b, H, d = q.shape
+    B.qk_norm_rope(q, k, None, q_out, k_out, None, norm.q_weight, norm.k_weight, norm.eps, b, H, 1,
+                   H * d, d, d, d, d, 1, d, meta.pos, meta.L_meta, 0, cache.cur_tok, None, theta,
+                   status=cache.status, stream=stream)
+
+
+def _normed(norm, q, k_new, cache, meta, theta, stream):
+    """The q, k and rotary base that a decode call gets: with a norm, q and k
+    are normalised and rotated ahead of it."""
+    if norm is None:
+        return q, k_new, theta
+    qs, ks = norm.step_buffers(q)
+    norm_rope_step(q, k_new, qs, ks, norm, cache, meta, theta, stream=stream)
+    return qs, ks, 0.0
+
+
 def decode_layer(q, k_new, v_new, cache: KVCache, m: int, meta: SpanMeta, ws: Workspace, o,
-                 scale=None, theta: float = 0.0, stream=None):
+                 scale=None, theta: float = 0.0, stream=None, norm: QKNorm = None):
     d = q.shape[-1]
+    if norm is not None:
+        q, k_new, theta = _normed(norm, q, k_new, cache, meta, theta, stream)
     B.compacted_decode_attn(q, k_new, v_new, cache.k(m), cache.v(m), cache.kv_len, cache.cur_tok,
                             meta.vu, meta.pos, meta.L_meta, o, cache.b, cache.H, cache.L_cap, d,
                             default_scale(d) if scale is None else scale, theta, ws.decode,
                             cache.status, stream=stream)
+
+
+def decode_weights_layer(q, k_new, v_new, cache: KVCache, m: int, meta: SpanMeta, ws: Workspace,
+                         o, w_in=None, w_out=None, scale=None, theta: float = 0.0, stream=None,
+                         norm: QKNorm = None):
+    """decode_layer that adds the weight the step gives each row: w_out = w_in
+    + weights, (b, H, L_cap) fp32, by default in place on the cache's own
+    sums (track_weights)."""
+    d = q.shape[-1]
+    if w_out is None:
+        w_in = w_out = cache._w[m]
+    q, k_new, theta = _normed(norm, q, k_new, cache, meta, theta, stream)
+    B.compacted_decode_attn_weights(q, k_new, v_new, cache.k(m), cache.v(m), cache.kv_len,
+                                    cache.cur_tok, meta.vu, meta.pos, meta.L_meta, o, w_in, w_out,
+                                    cache.b, cache.H, cache.L_cap, d,
+                                    default_scale(d) if scale is None else scale, theta,
+                                    ws.weights, cache.status, stream=stream)
+
+
+def prompt_weights(q, cache: KVCache, m: int, meta: SpanMeta, ws: Workspace, tok0: int, w_in=None,
+                   w_out=None, scale=None, stream=None):
+    """Adds the weight that queries q (b, H, nq, d), tokens tok0.., give each
+    row of layer m that the cache holds: w_out = w_in + weights, by default in
+    place on the cache's own sums (track_weights).  q is rotated as the keys
+    are; its last queries alone make a vote of recent tokens."""
+    b, H, nq, d = q.shape
+    if w_out is None:
+        w_in = w_out = cache._w[m]
+    B.cached_attn_weights(q, cache.k(m), w_in, w_out, b, H, nq, d, q.stride(1),
+                          cache.k(m).stride(1), default_scale(d) if scale is None else scale,
+                          meta.vu, meta.L_meta, tok0, cache.kv_len, cache.tok_idx, cache.L_cap,
+                          ws.weights, stream=stream)
+
+
+def shared_decode_layer(q, k_new, v_new, prefix: KVCache, cache: KVCache, m: int, meta: SpanMeta,
+                        ws: Workspace, o, scale=None, theta: float = 0.0, stream=None,
+                        norm: QKNorm = None):
+    """decode_layer for sequences that continue shared prefixes: sequence s
+    attends over the rows of prefix s // (cache.b / prefix.b), read once for
+    all its sequences, and over its own rows."""
+    d = q.shape[-1]
+    q, k_new, theta = _normed(norm, q, k_new, cache, meta, theta, stream)
+    B.shared_prefix_decode_attn(q, k_new, v_new, prefix.k(m), prefix.v(m), prefix.kv_len,
+                                prefix.b, prefix.L_cap, cache.k(m), cache.v(m), cache.kv_len,
+                                cache.cur_tok, meta.vu, meta.pos, meta.L_meta, o, cache.b,
+                                cache.H, cache.L_cap, d,
+                                default_scale(d) if scale is None else scale, theta, ws.shared,
+                                cache.status, stream=stream)
 
 
 def prefill_block(q, cache: KVCache, m: int, o, meta: SpanMeta, ws: Workspace, tok0: int, row0,
@@ -178,7 +350,7 @@ def prefill_block_plan(cache: KVCache, meta: SpanMeta, ws: Workspace, tok0: int,
 
 def prefill_progressive(q, k, v, o, cache: KVCache, meta: SpanMeta, ws: Workspace, L: int,
                         block: int, theta: float = 0.0, scale=None, stream=None,
-                        on_block=None):
+                        on_block=None, norm: QKNorm = None, evict=None):
     """Process the prompt (tokens 0..L-1) in blocks of `block` tokens:
     for each block, append its rows to the compacted cache (keys rotated),
     run the masked attention of its queries over the cache for every layer,
@@ -187,9 +359,17 @@ def prefill_progressive(q, k, v, o, cache: KVCache, meta: SpanMeta, ws: Workspac
     q, k, v, o: (M, b, H, >= L, d) per-layer prompt tensors (o receives the
     outputs).  The cache starts empty; at the end it holds the rows a token
     after the prompt may see, exactly as a one-shot prefill + compaction
-    leaves it.  on_block(B1), if given, is called after each block."""
+    leaves it.  on_block(B1), if given, is called after each block.
+
+    norm: normalises q and k by the head before they are rotated.  evict =
+    (heavy, recent): each block's queries add to the rows' accumulated weights
+    (cache.track_weights, a workspace with weights >= block) and the rows
+    beyond that budget leave after the block, so the cache needs room for
+    heavy + recent + block rows and later blocks attend over what is left."""
     M, b, H, _, d = q.shape
     cache.kv_len.zero_()
+    if evict is not None:
+        cache.w.zero_()
     row0 = torch.empty(b, dtype=torch.int32, device=q.device)
     nxt = torch.empty(b, dtype=torch.int32, device=q.device)
     qr = torch.empty(b, H, block, d, dtype=q.dtype, device=q.device)
@@ -200,13 +380,22 @@ def prefill_progressive(q, k, v, o, cache: KVCache, meta: SpanMeta, ws: Workspac
         for m in range(M):
             qb, kb, vb = (x[m, :, :, B0:B0 + n] for x in (q, k, v))
             dst = cache.k(m)
-            B.rope_block(qb, kb, vb, qr, dst, cache.v(m), row0, cache.L_cap, b, H, n,
-                         qb.stride(1), kb.stride(1), vb.stride(1), qr.stride(1), dst.stride(1), d,
-                         meta.pos, meta.L_meta, B0, theta, status=cache.status, stream=stream)
+            if norm is not None:
+                norm_rope_rows(qb, kb, vb, qr[:, :, :n], dst, cache.v(m), norm, meta, n, B0, theta,
+                               row0=row0, status=cache.status, stream=stream)
+            else:
+                B.rope_block(qb, kb, vb, qr, dst, cache.v(m), row0, cache.L_cap, b, H, n,
+                             qb.stride(1), kb.stride(1), vb.stride(1), qr.stride(1), dst.stride(1),
+                             d, meta.pos, meta.L_meta, B0, theta, status=cache.status,
+                             stream=stream)
             prefill_block(qr[:, :, :n], cache, m, o[m, :, :, B0:B0 + n], meta, ws, B0, row0,
                           scale=scale, stream=stream, planned=True)
+            if evict is not None:
+                prompt_weights(qr[:, :, :n], cache, m, meta, ws, B0, scale=scale, stream=stream)
         nxt.fill_(B0 + n)
         cache.compact(meta, next_tok=nxt, stream=stream)
+        if evict is not None:
+            cache.evict(*evict, stream=stream)
         if on_block is not None:
             on_block(B0 + n)
     cache.cur_tok.fill_(L)
