@@ -132,6 +132,71 @@ __device__ __forceinline__ void load_rotated_piece(const T* x, int seg, bool rot
   }
 }
 
+// What a launch does beside the step itself.
+struct StepOnly {
+  static constexpr bool WEIGHTS = false, PREFIX = false;
+};
+// Adds the step's softmax weights to each row's accumulated weight.  A row's
+// weight needs the whole slice's maximum and sum, so the scores (log2 units)
+// are kept in `scores` and turned into weights once those are known: by the
+// slice's own workgroup where there is one, else by workgroups of the merge.
+// 4 bytes written and 4 read a row (mostly from the L2) beside the 4 * d that
+// the row itself takes in bf16; computing the scores again would read the keys
+// twice.
+struct StepWeights {
+  static constexpr bool WEIGHTS = true, PREFIX = false;
+  const float* w_in;
+  float* w_out;
+  float* scores;  // [slice][L_cap]
+};
+// Joins the partials of a shared prefix (one per chunk of it) to the slice's.
+struct StepPrefix {
+  static constexpr bool WEIGHTS = false, PREFIX = true;
+  const float* o;    // [slice][n][d], unnormalised
+  const float2* ml;  // [slice][n]: maximum (log2 units), sum of weights
+  int32_t n;
+};
+
+// w_out of rows [0, n) of a slice whose step adds nothing
+__device__ __forceinline__ void keep_weights(const StepWeights& x, int64_t at, int n, int tid,
+                                             int nthr) {
+  for (int r = tid; r < n; r += nthr) x.w_out[at + r] = x.w_in ? x.w_in[at + r] : 0.f;
+}
+
+// w_out of rows [r0, r1) of a slice of n cache rows and the new one, from the
+// slice's maximum M (log2 units) and sum of weights L
+__device__ __forceinline__ void add_weights(const StepWeights& x, int64_t at, int n, int r0, int r1,
+                                            float M, float L, int tid, int nthr) {
+  const float inv = 1.f / L;
+#pragma unroll 4
+  for (int r = r0 + tid; r < r1; r += nthr) {
+    const float old = x.w_in && r < n ? x.w_in[at + r] : 0.f;
+    x.w_out[at + r] = fmaf(exp2f(x.scores[at + r] - M), inv, old);
+  }
+}
+
+// element e's share of the prefix partials joined to a slice's maximum M, sum
+// L and unnormalised output ov
+template <int D>
+__device__ __forceinline__ void join_prefix(const StepPrefix& x, int bh, int e, float& M, float& L,
+                                            float& ov) {
+  const float* o = x.o + (int64_t)bh * x.n * D;
+  const float2* ml = x.ml + (int64_t)bh * x.n;
+  float Mx = M;
+#pragma unroll 4
+  for (int c = 0; c < x.n; ++c) Mx = fmaxf(Mx, ml[c].x);
+  const float f = exp2f(M - Mx);  // M is finite: the slice holds the new row
+  L *= f;
+  ov *= f;
+#pragma unroll 4
+  for (int c = 0; c < x.n; ++c) {
+    const float w = exp2f(ml[c].x - Mx);  // 0 for a chunk without rows (its maximum -inf)
+    L = fmaf(ml[c].y, w, L);
+    ov = fmaf(o[c * D + e], w, ov);
+  }
+  M = Mx;
+}
+
 // 0: ordinary append step; 1: <CL> step; 2: token outside [0, L_meta);
 // 3: no room for the new row
 __device__ __forceinline__ int step_kind(const int32_t* cur_tok, const int32_t* vu,
@@ -189,14 +254,14 @@ __device__ __forceinline__ void write_special(int kind, const T* v_new, T* o, in
 
 // FINAL: the workgroup covers the whole slice (one chunk) and
 // writes the output itself; otherwise it writes a partial for the combine.
-template <typename T, int D, int THREADS, bool FINAL>
+template <typename T, int D, int THREADS, bool FINAL, typename X>
 __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
     const T* __restrict__ q, const T* __restrict__ k_new, const T* __restrict__ v_new,
     T* __restrict__ k_cache, T* __restrict__ v_cache, const int32_t* __restrict__ kv_len,
     const int32_t* __restrict__ cur_tok, const int32_t* __restrict__ vu,
     const int32_t* __restrict__ pos, int32_t L_meta, int32_t H, int32_t L_cap, float qscale,
     int rotate, RopeTab tab, float* __restrict__ part, int32_t n_chunk_max, int32_t n_work,
-    Split sp, T* __restrict__ o, int32_t* __restrict__ status) {
+    Split sp, T* __restrict__ o, int32_t* __restrict__ status, X x) {
   using C = DecCfg<T, D, THREADS>;
   constexpr int E = C::E, LPR = C::LPR, GRP = C::GRP, RPW = C::RPW, U = C::U, NG = C::NG;
   // chunk-major order: every slice's first chunk is dispatched before any
@@ -209,6 +274,8 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
   const int kind = step_kind(cur_tok, vu, kv_len, s, L_meta, L_cap);
   if (kind != 0) {  // the combine handles it, or this workgroup when FINAL
     if constexpr (FINAL) write_special<T, D>(kind, v_new, o, status, bh, H, threadIdx.x, THREADS);
+    if constexpr (FINAL && X::WEIGHTS)
+      keep_weights(x, (int64_t)bh * L_cap, min(max(kv_len[s], 0), L_cap), threadIdx.x, THREADS);
     return;
   }
   const int n = kv_len[s];
@@ -275,7 +342,10 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
 #pragma unroll
       for (int e = 0; e < E; ++e) d = fmaf(qf[e], kf[e], d);
       d = group_sum<GRP>(d);
-      sc[u] = (base + u * RPW + g < rc) ? d : -INFINITY;
+      const int row = base + u * RPW + g;
+      sc[u] = row < rc ? d : -INFINITY;
+      if constexpr (X::WEIGHTS)
+        if (row < rc && seg == 0) x.scores[(int64_t)bh * L_cap + row] = d;
     }
     float mx = m;
 #pragma unroll
@@ -314,6 +384,8 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
 #pragma unroll
     for (int e = 0; e < E; ++e) d = fmaf(qf[e], kf[e], d);
     d = group_sum<GRP>(d);
+    if constexpr (X::WEIGHTS)
+      if (seg == 0) x.scores[(int64_t)bh * L_cap + n] = d;
     const float mx = fmaxf(m, d);
     const float alpha = exp2f(m - mx);
     const float p = exp2f(d - mx);
@@ -339,7 +411,8 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
   }
   __syncthreads();
   __shared__ float res[D];
-  if (tid < D) {
+  if (X::WEIGHTS || tid < D) {  // with weights every thread takes the maximum and the sum
+    const int e = min(tid, D - 1);
     float M = -INFINITY;
     for (int i = 0; i < NG; ++i) M = fmaxf(M, sm[i]);
     float Lsum = 0.f, ov = 0.f;
@@ -347,9 +420,13 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
       if (sm[i] == -INFINITY) continue;
       const float w = exp2f(sm[i] - M);
       Lsum += sl[i] * w;
-      ov += sacc[i][tid] * w;
+      ov += sacc[i][e] * w;
     }
-    if constexpr (FINAL) {
+    if constexpr (FINAL && X::PREFIX) join_prefix<D>(x, bh, tid, M, Lsum, ov);
+    if constexpr (FINAL && X::WEIGHTS)
+      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, M, Lsum, tid, THREADS);
+    if (tid >= D) {
+    } else if constexpr (FINAL) {
       res[tid] = ov / Lsum;
     } else {
       float* out = part + ((int64_t)bh * n_chunk_max + chunk) * (D + 2);
@@ -373,13 +450,16 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
 // adds chunks w, w + 4, ..., the output elements spread over its lanes; the
 // waves' sums meet in LDS).
 constexpr int COMBINE_WAVES = 4;
-template <typename T, int D>
+constexpr int WEIGHT_ROWS = 2048;  // rows of a workgroup that only adds weights
+template <typename T, int D, typename X>
 __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
     const T* __restrict__ v_new, const int32_t* __restrict__ kv_len,
     const int32_t* __restrict__ cur_tok, const int32_t* __restrict__ vu, int32_t L_meta,
     int32_t H, FastDiv by_H, int32_t L_cap, const float* __restrict__ part, int32_t n_chunk_max,
-    Split sp, T* __restrict__ o, int32_t* __restrict__ status, int32_t ring) {
-  const int bh = blockIdx.x;
+    Split sp, T* __restrict__ o, int32_t* __restrict__ status, int32_t ring, int32_t n_bh, X x) {
+  // the workgroups behind the slices' add weights, WEIGHT_ROWS rows each
+  const int blk = X::WEIGHTS ? (int)blockIdx.x / n_bh : 0;
+  const int bh = (int)blockIdx.x - blk * n_bh;
   const int s = fast_div(bh, by_H);
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -400,10 +480,30 @@ __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
                    : (ring == 0 && (n < 0 || n >= L_cap))       ? 3
                                                                 : 0;
   if (kind != 0) {
-    write_special<T, D>(kind, v_new, o, status, bh, H, tid, 64 * COMBINE_WAVES);
+    if (blk == 0) write_special<T, D>(kind, v_new, o, status, bh, H, tid, 64 * COMBINE_WAVES);
+    if constexpr (X::WEIGHTS)
+      if (blk == 1) keep_weights(x, (int64_t)bh * L_cap, min(max(n, 0), L_cap), tid, 64 * COMBINE_WAVES);
     return;
   }
   const int nch = chunk_plan(n + 1, sp).n;
+  if constexpr (X::WEIGHTS) {
+    if (blk > 0) {
+      const int r0 = (blk - 1) * WEIGHT_ROWS;
+      if (r0 > n) return;
+      float Mw = -INFINITY, lw = 0.f;
+      for (int c0 = 0; c0 < nch; c0 += 64) {
+        const int c = c0 + lane;
+        const float mc = c >= nch ? -INFINITY : c0 == 0 ? m0 : p[c * (D + 2)];
+        const float lc = c >= nch ? 0.f : c0 == 0 ? l0 : p[c * (D + 2) + 1];
+        const float mn = fmaxf(Mw, wave_max(mc));
+        lw = lw * exp2f(Mw - mn) + wave_sum(lc * exp2f(mc - mn));
+        Mw = mn;
+      }
+      add_weights(x, (int64_t)bh * L_cap, n, r0, min(r0 + WEIGHT_ROWS, n + 1), Mw, lw, tid,
+                  64 * COMBINE_WAVES);
+      return;
+    }
+  }
   constexpr int PER = (D + 63) / 64;  // output elements per lane
   float M = -INFINITY, lsum = 0.f, acc[PER];
 #pragma unroll
@@ -443,6 +543,7 @@ __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < COMBINE_WAVES; ++w) v += sums[w][tid];
+    if constexpr (X::PREFIX) join_prefix<D>(x, bh, tid, M, lsum, v);
     v /= lsum;
     if constexpr (sizeof(T) == 2) o[(int64_t)bh * D + tid] = f32_to_bf16(v);
     else o[(int64_t)bh * D + tid] = v;
@@ -513,7 +614,7 @@ constexpr int half_wave_count() {
   else return half_wave_count<NV, MASK / 2>();
 }
 
-template <int D, int NW, bool FINAL, bool SPEC2 = false>
+template <int D, int NW, bool FINAL, bool SPEC2, typename X>
 __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k_new,
     const uint16_t* __restrict__ v_new, uint16_t* __restrict__ k_cache,
@@ -522,7 +623,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     const int32_t* __restrict__ pos, int32_t L_meta, int32_t H, int32_t L_cap, float qscale,
     int rotate, RopeTab tab, float* __restrict__ part, int32_t n_chunk_max, FastDiv by_H,
     FastDiv by_slices, int32_t n_bh, Split sp, uint16_t* __restrict__ o,
-    int32_t* __restrict__ status, int32_t ring) {
+    int32_t* __restrict__ status, int32_t ring, X x) {
   constexpr int KS = D / 16;     // k steps of 16 elements
   constexpr int NA = 8 * KS;     // value elements per lane
   constexpr int THREADS = NW * 64;
@@ -634,6 +735,8 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                    : (vu_t == t_raw ? 1 : ((ring == 0 && (n_raw < 0 || n_raw >= L_cap)) ? 3 : 0));
   if (kind != 0) {
     if constexpr (FINAL) write_special<uint16_t, D>(kind, v_new, o, status, bh, H, tid, THREADS);
+    if constexpr (FINAL && X::WEIGHTS)
+      keep_weights(x, (int64_t)bh * L_cap, min(max(n_raw, 0), L_cap), tid, THREADS);
     return;
   }
   if (chunk >= cp.n) return;
@@ -669,7 +772,11 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
   }
   __syncthreads();
 
-  bf16x8 qhi[KS], qlo[KS];
+  // Accumulated weights are fp32 sums: their launches carry q's last 8 bits
+  // too, in a third term (two leave 2^-17 of a score).  There the three terms
+  // lie in rows 0, 1 and 2 (mod 4) of one A operand: a lane's first three
+  // results are its key's products with them, one MFMA a k step.
+  bf16x8 qhi[KS], qlo[X::WEIGHTS ? 1 : KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
     u32x4 wh, wl;
@@ -679,9 +786,15 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
       const uint32_t hw = pack_bf16x2(x0, x1);
       wh[i] = hw;
       wl[i] = pack_bf16x2(x0 - bf16_lo(hw), x1 - bf16_hi(hw));
+      if constexpr (X::WEIGHTS) {
+        const uint32_t we = pack_bf16x2(x0 - bf16_lo(hw) - bf16_lo(wl[i]),
+                                        x1 - bf16_hi(hw) - bf16_hi(wl[i]));
+        const int term = kr & 3;
+        wh[i] = term == 0 ? hw : term == 1 ? wl[i] : term == 2 ? we : 0;
+      }
     }
     qhi[kk] = __builtin_bit_cast(bf16x8, wh);
-    qlo[kk] = __builtin_bit_cast(bf16x8, wl);
+    if constexpr (!X::WEIGHTS) qlo[kk] = __builtin_bit_cast(bf16x8, wl);
   }
 
   float M = -INFINITY, l = 0.f, acc[NA];
@@ -707,10 +820,13 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     for (int kk = 0; kk < KS; ++kk) {
       const bf16x8 kv = __builtin_bit_cast(bf16x8, kd[kk]);
       c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qhi[kk], kv, c, 0, 0, 0);
-      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qlo[kk], kv, c, 0, 0, 0);
+      if constexpr (!X::WEIGHTS) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qlo[kk], kv, c, 0, 0, 0);
     }
+    if constexpr (X::WEIGHTS) c[0] += c[1] + c[2];
     const int row = r0 + 32 * i + kr;
     const float sc = (row < rc && row != slot) ? c[0] * qscale : -INFINITY;
+    if constexpr (X::WEIGHTS)
+      if (h == 0 && row < rc) x.scores[(int64_t)bh * L_cap + row] = sc;
     const float p = weigh(sc);
     if (h == 0) l += p;
 #pragma unroll
@@ -730,8 +846,11 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
   if (holds_new && wave == 0) {
     float prod = kqs[lane];
     if (lane + 64 < D) prod += kqs[lane + 64];
-    const float p = weigh(wave_sum(prod) * qscale);
+    const float sc = wave_sum(prod) * qscale;
+    const float p = weigh(sc);
     if (lane == 0) l += p;
+    if constexpr (X::WEIGHTS)
+      if (lane == 0) x.scores[(int64_t)bh * L_cap + n] = sc;
     if (kr == 0) {
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
@@ -774,7 +893,8 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
   }
   if (lane == 0) { sm[wave] = M; sl[wave] = l; }
   __syncthreads();
-  if (tid < D) {
+  if (X::WEIGHTS || tid < D) {  // with weights every thread takes the maximum and the sum
+    const int e = min(tid, D - 1);
     float Mx = -INFINITY;
 #pragma unroll
     for (int w = 0; w < NW; ++w) Mx = fmaxf(Mx, sm[w]);
@@ -784,9 +904,13 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
       const float f = exp2f(sm[w] - Mx);
       const bool any = sm[w] != -INFINITY;  // the wave had a row
       Ls += any ? sl[w] * f : 0.f;
-      ov += any ? sacc[w][tid] * f : 0.f;
+      ov += any ? sacc[w][e] * f : 0.f;
     }
-    if constexpr (FINAL) {
+    if constexpr (FINAL && X::PREFIX) join_prefix<D>(x, bh, tid, Mx, Ls, ov);
+    if constexpr (FINAL && X::WEIGHTS)
+      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, Mx, Ls, tid, THREADS);
+    if (tid >= D) {
+    } else if constexpr (FINAL) {
       o[(int64_t)bh * D + tid] = f32_to_bf16(ov / Ls);
     } else {
       float* out = part + ((int64_t)bh * n_chunk_max + chunk) * (D + 2);
@@ -805,13 +929,13 @@ static bool one_workgroup(bool bf16, int64_t slices, int L_cap) {
 
 static int n_chunks(int L_cap) { return (L_cap + DEC_CH - 1) / DEC_CH; }
 
-template <typename T, int D>
+template <typename T, int D, typename X = StepOnly>
 static int launch_decode(const void* q, const void* k_new, const void* v_new, void* k_cache,
                          void* v_cache, const int32_t* kv_len, const int32_t* cur_tok,
                          const int32_t* vu, const int32_t* pos, int32_t L_meta, void* o,
                          int32_t b, int32_t H, int32_t L_cap, float scale, float theta,
                          void* ws, size_t ws_bytes, int32_t* status, hipStream_t stream,
-                         int32_t ring = 0) {
+                         int32_t ring = 0, X x = X()) {
   RopeTab tab;
   for (int i = 0; i < 40; ++i) tab.w[i] = 0.0;
   const int rotate = theta > 0.f ? 1 : 0;
@@ -844,9 +968,9 @@ static int launch_decode(const void* q, const void* k_new, const void* v_new, vo
       // for nothing, never used).
       const bool spec2 = ring == 0 && (int64_t)L_cap >= (int64_t)DEC_SPEC2_ROWS * nw;
 #define SCKV_DECODE_LAUNCH(DD, NWW, SP)                                                          \
-  decode_mfma_kernel<DD, NWW, true, SP><<<slices, NWW * 64, 0, stream>>>(                         \
+  decode_mfma_kernel<DD, NWW, true, SP, X><<<slices, NWW * 64, 0, stream>>>(                      \
       qq, kn, vn, kc, vc, kv_len, cur_tok, vu, pos, L_meta, H, L_cap, qs, rotate, tab, part, 1,  \
-      by_H, by_slices, slices, Split{1, 1}, out, status, ring)
+      by_H, by_slices, slices, Split{1, 1}, out, status, ring, x)
       constexpr int D1 = D <= 64 ? D : 64;  // nw == 1 only where D <= 64
       if (nw == 1 && spec2) SCKV_DECODE_LAUNCH(D1, 1, true);
       else if (nw == 1) SCKV_DECODE_LAUNCH(D1, 1, false);
@@ -857,13 +981,13 @@ static int launch_decode(const void* q, const void* k_new, const void* v_new, vo
 #undef SCKV_DECODE_LAUNCH
     } else {
       if (narrow)
-        decode_chunk_kernel<T, D, 256, true><<<slices, 256, 0, stream>>>(
+        decode_chunk_kernel<T, D, 256, true, X><<<slices, 256, 0, stream>>>(
             qq, kn, vn, kc, vc, kv_len, cur_tok, vu, pos, L_meta, H, L_cap, qs, rotate, tab, part,
-            1, slices, Split{1, 1}, out, status);
+            1, slices, Split{1, 1}, out, status, x);
       else
-        decode_chunk_kernel<T, D, 512, true><<<slices, 512, 0, stream>>>(
+        decode_chunk_kernel<T, D, 512, true, X><<<slices, 512, 0, stream>>>(
             qq, kn, vn, kc, vc, kv_len, cur_tok, vu, pos, L_meta, H, L_cap, qs, rotate, tab, part,
-            1, slices, Split{1, 1}, out, status);
+            1, slices, Split{1, 1}, out, status, x);
     }
     return hip_check(hipGetLastError(), "compacted_decode_attn: launch");
   }
@@ -875,17 +999,18 @@ static int launch_decode(const void* q, const void* k_new, const void* v_new, vo
   const Split sp{want, nc};
   const int n_work = slices * nc;
   if constexpr (sizeof(T) == 2)
-    decode_mfma_kernel<D, 4, false><<<n_work, 256, 0, stream>>>(
+    decode_mfma_kernel<D, 4, false, false, X><<<n_work, 256, 0, stream>>>(
         qq, kn, vn, kc, vc, kv_len, cur_tok, vu, pos, L_meta, H, L_cap, qs, rotate, tab, part, nc,
-        by_H, by_slices, slices, sp, out, status, ring);
+        by_H, by_slices, slices, sp, out, status, ring, x);
   else
-    decode_chunk_kernel<T, D, DEC_THREADS, false><<<n_work, DEC_THREADS, 0, stream>>>(
+    decode_chunk_kernel<T, D, DEC_THREADS, false, X><<<n_work, DEC_THREADS, 0, stream>>>(
         qq, kn, vn, kc, vc, kv_len, cur_tok, vu, pos, L_meta, H, L_cap, qs, rotate, tab, part, nc,
-        n_work, sp, out, status);
+        n_work, sp, out, status, x);
   int rc = hip_check(hipGetLastError(), "compacted_decode_attn: chunk launch");
   if (rc) return rc;
-  decode_combine_kernel<T, D><<<slices, 64 * COMBINE_WAVES, 0, stream>>>(
-      vn, kv_len, cur_tok, vu, L_meta, H, by_H, L_cap, part, nc, sp, out, status, ring);
+  const int wblk = X::WEIGHTS ? (int)((L_cap + (int64_t)WEIGHT_ROWS - 1) / WEIGHT_ROWS) : 0;
+  decode_combine_kernel<T, D, X><<<slices * (1 + wblk), 64 * COMBINE_WAVES, 0, stream>>>(
+      vn, kv_len, cur_tok, vu, L_meta, H, by_H, L_cap, part, nc, sp, out, status, ring, slices, x);
   return hip_check(hipGetLastError(), "compacted_decode_attn: combine launch");
 }
 
@@ -956,20 +1081,20 @@ static int decode_checks(const char* W, const void* q, const void* k_new, const 
   return SCKV_OK;
 }
 
+template <typename X = StepOnly>
 static int decode_dispatch(const void* q, const void* k_new, const void* v_new, void* k_cache,
                            void* v_cache, const int32_t* kv_len, const int32_t* cur_tok,
                            const int32_t* vu, const int32_t* pos, int32_t L_meta, void* o,
                            int32_t b, int32_t H, int32_t L_cap, int32_t d_head, sckv_dtype dt,
                            float scale, float rope_theta, void* ws, size_t ws_bytes,
-                           int32_t* status, hipStream_t stream) {
+                           int32_t* status, hipStream_t stream, X x = X()) {
   const int32_t* p = pos ? pos : vu;  // pos is read only when rotating
-  if (dt == SCKV_BF16)
-    return d_head == 64
-               ? launch_decode<uint16_t, 64>(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, p, L_meta, o, b, H, L_cap, scale, rope_theta, ws, ws_bytes, status, stream)
-               : launch_decode<uint16_t, 80>(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, p, L_meta, o, b, H, L_cap, scale, rope_theta, ws, ws_bytes, status, stream);
-  return d_head == 64
-             ? launch_decode<float, 64>(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, p, L_meta, o, b, H, L_cap, scale, rope_theta, ws, ws_bytes, status, stream)
-             : launch_decode<float, 80>(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, p, L_meta, o, b, H, L_cap, scale, rope_theta, ws, ws_bytes, status, stream);
+#define SCKV_DISPATCH(T, DD)                                                                       \
+  launch_decode<T, DD, X>(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, p, L_meta, o, b, \
+                          H, L_cap, scale, rope_theta, ws, ws_bytes, status, stream, 0, x)
+  if (dt == SCKV_BF16) return d_head == 64 ? SCKV_DISPATCH(uint16_t, 64) : SCKV_DISPATCH(uint16_t, 80);
+  return d_head == 64 ? SCKV_DISPATCH(float, 64) : SCKV_DISPATCH(float, 80);
+#undef SCKV_DISPATCH
 }
 
 extern "C" int compacted_decode_attn(const void* q, const void* k_new, const void* v_new,
@@ -1054,4 +1179,93 @@ extern "C" int compacted_decode_attn_noalloc(const void* q, const void* k_new, c
   if (rc) return rc;
   return decode_dispatch(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos, L_meta, o, b,
                          H, L_cap, d_head, dt, scale, rope_theta, ws, need, status, stream);
+}
+
+// ---------------------------------------------------------------------------
+// the step that also adds its weights; ws: chunk partials, then the scores
+// ---------------------------------------------------------------------------
+// Bytes of the partials: what a split launch needs at least, and room for the
+// DEC_FILL workgroups that a launch of few slices is cut into.
+static size_t partial_bytes(int32_t b, int32_t H, int32_t L_cap, int32_t d_head) {
+  const size_t fine = (size_t)DEC_FILL * (d_head + 2) * sizeof(float);
+  return (std::max(sckv_decode_workspace_bytes(b, H, L_cap, d_head), fine) + 15) / 16 * 16;
+}
+
+extern "C" size_t sckv_decode_weights_workspace_bytes(int32_t b, int32_t H, int32_t L_cap,
+                                                      int32_t d_head) {
+  if (b <= 0 || H <= 0 || L_cap <= 0 || d_head <= 0) return 0;
+  return partial_bytes(b, H, L_cap, d_head) + (size_t)b * H * L_cap * sizeof(float);
+}
+
+extern "C" int compacted_decode_attn_weights(
+    const void* q, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
+    const int32_t* kv_len, const int32_t* cur_tok, const int32_t* vu, const int32_t* pos,
+    int32_t L_meta, void* o, const float* w_in, float* w_out, int32_t b, int32_t H, int32_t L_cap,
+    int32_t d_head, sckv_dtype dt, float scale, float rope_theta, void* ws, size_t ws_bytes,
+    int32_t* status, hipStream_t stream) {
+  clear_error();
+  const std::string W = "compacted_decode_attn_weights";
+  const int rc = decode_checks(W.c_str(), q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu,
+                               pos, L_meta, o, b, H, L_cap, d_head, dt, scale, rope_theta);
+  if (rc) return rc;
+  if (!w_out || !ws) return fail(SCKV_EINVAL, W + ": null pointer");
+  if (!aligned4(w_out) || !aligned4(w_in))
+    return fail(SCKV_EINVAL, W + ": w_in and w_out must be 4-byte aligned");
+  if (!aligned16(ws)) return fail(SCKV_EINVAL, W + ": buffers must be 16-byte aligned");
+  if (ws_bytes < sckv_decode_weights_workspace_bytes(b, H, L_cap, d_head))
+    return fail(SCKV_EINVAL, W + ": workspace too small");
+  const size_t part = partial_bytes(b, H, L_cap, d_head);
+  const StepWeights x = {w_in, w_out, reinterpret_cast<float*>(static_cast<char*>(ws) + part)};
+  return decode_dispatch(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos, L_meta, o, b,
+                         H, L_cap, d_head, dt, scale, rope_theta, ws, part, status, stream, x);
+}
+
+// ---------------------------------------------------------------------------
+// the step behind shared prefixes; ws: chunk partials of the own rows, then
+// the prefixes' partials
+// ---------------------------------------------------------------------------
+// (the size function is not told the element type)
+static int most_chunks(int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap) {
+  return std::max(prefix_chunks(true, n_prefix, H, per, P_cap),
+                  prefix_chunks(false, n_prefix, H, per, P_cap));
+}
+
+extern "C" size_t sckv_shared_decode_workspace_bytes(int32_t b, int32_t H, int32_t n_prefix,
+                                                     int32_t P_cap, int32_t L_cap,
+                                                     int32_t d_head) {
+  if (b <= 0 || H <= 0 || n_prefix <= 0 || P_cap <= 0 || L_cap <= 0 || d_head <= 0 || b % n_prefix)
+    return 0;
+  return partial_bytes(b, H, L_cap, d_head) +
+         (size_t)b * H * most_chunks(n_prefix, H, b / n_prefix, P_cap) * (d_head + 2) * sizeof(float);
+}
+
+extern "C" int shared_prefix_decode_attn(
+    const void* q, const void* k_new, const void* v_new, const void* k_prefix,
+    const void* v_prefix, const int32_t* prefix_len, int32_t n_prefix, int32_t P_cap,
+    void* k_cache, void* v_cache, const int32_t* kv_len, const int32_t* cur_tok,
+    const int32_t* vu, const int32_t* pos, int32_t L_meta, void* o, int32_t b, int32_t H,
+    int32_t L_cap, int32_t d_head, sckv_dtype dt, float scale, float rope_theta, void* ws,
+    size_t ws_bytes, int32_t* status, hipStream_t stream) {
+  clear_error();
+  const std::string W = "shared_prefix_decode_attn";
+  int rc = decode_checks(W.c_str(), q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos,
+                         L_meta, o, b, H, L_cap, d_head, dt, scale, rope_theta);
+  if (rc) return rc;
+  if (!k_prefix || !v_prefix || !prefix_len || !ws) return fail(SCKV_EINVAL, W + ": null pointer");
+  if (n_prefix <= 0 || P_cap <= 0 || b % n_prefix)
+    return fail(SCKV_EINVAL, W + ": b must be a multiple of n_prefix, sizes positive");
+  if (!aligned16(k_prefix) || !aligned16(v_prefix) || !aligned16(ws))
+    return fail(SCKV_EINVAL, W + ": buffers must be 16-byte aligned");
+  if (ws_bytes < sckv_shared_decode_workspace_bytes(b, H, n_prefix, P_cap, L_cap, d_head))
+    return fail(SCKV_EINVAL, W + ": workspace too small");
+  const size_t own = partial_bytes(b, H, L_cap, d_head);
+  const int n = prefix_chunks(dt == SCKV_BF16, n_prefix, H, b / n_prefix, P_cap);
+  float* po = reinterpret_cast<float*>(static_cast<char*>(ws) + own);
+  float* ml = po + (size_t)b * H * n * d_head;
+  rc = launch_prefix(q, k_prefix, v_prefix, prefix_len, n_prefix, P_cap, cur_tok, pos ? pos : vu,
+                     L_meta, b, H, d_head, dt, scale, rope_theta, po, ml, stream);
+  if (rc) return rc;
+  const StepPrefix x = {po, reinterpret_cast<const float2*>(ml), n};
+  return decode_dispatch(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos, L_meta, o, b,
+                         H, L_cap, d_head, dt, scale, rope_theta, ws, own, status, stream, x);
 }

@@ -26,6 +26,15 @@ int launch_move(void* kv, void* kv_out, int32_t M, int32_t b, int32_t H, int32_t
                 int32_t d_head, sckv_dtype dt, const int32_t* kv_len, const int32_t* kept_src,
                 const char* what, hipStream_t stream);
 
+// the part of shared_prefix_decode_attn that reads the prefixes (shared.hip):
+// n = prefix_chunks(...) partials a slice, outputs [slice][n][d] in log2 units
+// and (maximum, sum) [slice][n][2]
+int prefix_chunks(bool bf16, int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap);
+int launch_prefix(const void* q, const void* k, const void* v, const int32_t* len,
+                  int32_t n_prefix, int32_t P_cap, const int32_t* cur_tok, const int32_t* pos,
+                  int32_t L_meta, int32_t b, int32_t H, int32_t d_head, sckv_dtype dt, float scale,
+                  float theta, float* part_o, float* part_ml, hipStream_t stream);
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline int elem_bytes(sckv_dtype dt) { return dt == SCKV_F32 ? 4 : 2; }

@@ -1,6 +1,25 @@
-// Decode steps that need more than one pass over a cache's rows in plain form:
-// the accumulated weights of a step, and attention over a shared prefix and
-// the sequence's own rows.
+// Attention of decode steps over a prefix that several sequences share
+// (several samples for one compressed document: Section 4.2), the part that
+// reads the prefix: each of its rows once for all of its sequences.
+//
+// Per (prefix, head) the queries of its sequences form a matrix, so the scores
+// S^T = K Q^T and the outputs O^T += V^T P^T are products on the matrix cores.
+// A wave takes one tile of 32 queries and 32-row blocks of keys; lane l owns
+// query l % 32 of S^T (16 of the block's 32 rows: 8a + 4(l/32) + c), hence the
+// running maximum and sum of a softmax in registers, and the same rows of P^T
+// are the B operand of the value product as they stand.  bf16 queries are
+// carried as two bf16 terms after the rotation (2^-17 of a score, as in the
+// decode step); the softmax weights are rounded to bf16 for the value product
+// (half a step of the output's own type a weight, averaged over the rows) and
+// their sum is that of the rounded ones.
+//
+// Bound by HBM while a tile of queries is not much larger than the card's
+// flops per byte; the workgroup's four key waves split its rows, and the rows
+// are split over workgroups (chunks) until the launch fills the CUs.  Each
+// chunk leaves one partial (maximum, sum, output) a query, which the step over
+// the sequences' own rows joins to its own at its end (decode.hip): two
+// launches a step.
+#include <algorithm>
 #include <cmath>
 #include <string>
 
@@ -8,239 +27,383 @@
 
 namespace sckv {
 
-struct StepFreq {
-  double w[40];
+constexpr int PRE_ROWS = 32;     // rows of a block
+constexpr int PRE_QUERIES = 32;  // queries of a tile
+constexpr int PRE_KEY_WAVES = 4;
+constexpr float PRE_RESCALE = 8.f;  // lazy maximum, log2 units
+
+struct PrefixFreq {
+  double w[40];  // theta^(-2i/d)
 };
 
-template <typename T>
-struct StepArgs {
-  const T *q, *k_new, *v_new, *k_pre, *v_pre;
-  T *k_cache, *v_cache, *o;
-  const int32_t *pre_len, *kv_len, *cur_tok, *vu, *pos;
-  const float* w_in;
-  float *w_out, *scores;
-  int32_t* status;
-  int32_t per, P_cap, L_meta, H, L_cap, rotate;
-  float c;
-};
-
-constexpr int STEP_THREADS = 256;
-
-// one workgroup per slice: scores of prefix rows, own rows and the new row,
-// their maximum and sum, then outputs and weights
+// The 16 scores and weights of a lane, the wave's tile of queries and its
+// outputs.  DB blocks of 32 output elements; in each, register v of lane l
+// holds element 8 (v/4) + 4 (l/32) + v % 4 of query l % 32.
 template <typename T, int D>
-__global__ __launch_bounds__(STEP_THREADS) void step_kernel(StepArgs<T> a, StepFreq tab) {
-  constexpr int E = Piece<T>::E;
-  __shared__ float qs[D], red[STEP_THREADS], acc[STEP_THREADS / 64][D];
-  const int bh = blockIdx.x, s = bh / a.H, h = bh % a.H, tid = threadIdx.x;
-  const int t = a.cur_tok[s];
-  const int len = a.kv_len[s];
-  const bool t_ok = t >= 0 && t < a.L_meta;
-  const int kind = !t_ok ? 2 : a.vu[(int64_t)s * a.L_meta + t] == t ? 1 : (len < 0 || len >= a.L_cap) ? 3 : 0;
-  const int n = min(max(len, 0), a.L_cap);
-  const int64_t wo = (int64_t)bh * a.L_cap;
-  T* o = a.o + (int64_t)bh * D;
-  if (kind != 0) {
-    if (kind > 1 && tid == 0 && h == 0 && a.status)
-      atomicOr(a.status, kind == 2 ? SCKV_STATUS_TOKEN : SCKV_STATUS_CAP);
-    for (int e = tid; e < D; e += STEP_THREADS) {
-      if (kind == 1) o[e] = a.v_new[(int64_t)bh * D + e];
-      else if constexpr (sizeof(T) == 2) o[e] = (T)0x7fc0;
-      else o[e] = NAN;
-    }
-    if (a.w_out)
-      for (int r = tid; r < n; r += STEP_THREADS) a.w_out[wo + r] = a.w_in ? a.w_in[wo + r] : 0.f;
-    return;
-  }
-  T* kc = a.k_cache + wo * D;
-  T* vc = a.v_cache + wo * D;
-  auto val = [](const T* p, int i) {
-    if constexpr (sizeof(T) == 2) return bf16_lo((uint32_t)p[i]);
-    else return p[i];
+struct PrefixTile {
+  static constexpr int DB = (D + 31) / 32;
+  static constexpr int KS = D / 16;
+  static constexpr int PITCH = 192;  // bytes of a value row in LDS: the transposing
+                                     // reads' 8 rows x 64 bytes then meet no bank twice
+  static constexpr int V_BYTES = sizeof(T) == 2 ? PRE_ROWS * PITCH : 0;
+  static constexpr int NK = sizeof(T) == 2 ? KS : D / 8;   // 16-byte pieces of a key row per lane
+  static constexpr int NV = sizeof(T) == 2 ? KS * 4 : 16 * DB;  // registers of a block's values
+  struct Rows {
+    u32x4 k[NK];
+    uint32_t v[NV];
   };
-  if (tid < D) {
-    const int64_t x = (int64_t)bh * D;
-    const int p = tid < D / 2 ? tid + D / 2 : tid - D / 2;
-    float qv = val(a.q + x, tid), kv = val(a.k_new + x, tid);
-    if (a.rotate) {
-      const double two_pi = 6.283185307179586476925286766559;
-      double ang = (double)a.pos[(int64_t)s * a.L_meta + t] * tab.w[tid < D / 2 ? tid : p];
-      ang -= two_pi * rint(ang / two_pi);
-      float sn, cs;
-      sincosf((float)ang, &sn, &cs);
-      if (tid < D / 2) sn = -sn;
-      qv = qv * cs + val(a.q + x, p) * sn;
-      kv = kv * cs + val(a.k_new + x, p) * sn;
-    }
-    qs[tid] = qv * a.c;
-    if constexpr (sizeof(T) == 2) kc[(int64_t)n * D + tid] = f32_to_bf16(kv);
-    else kc[(int64_t)n * D + tid] = kv;
-    vc[(int64_t)n * D + tid] = a.v_new[x + tid];
-  }
-  __threadfence_block();
-  __syncthreads();
-  const int g = s / a.per;
-  const int np = a.k_pre ? min(max(a.pre_len[g], 0), a.P_cap) : 0;
-  const int64_t po = ((int64_t)g * a.H + h) * a.P_cap * D;
-  const int rows = np + n + 1;
-  float* sc = a.scores + (int64_t)bh * ((int64_t)a.P_cap + a.L_cap);
-  float m = -INFINITY;
-  for (int r = tid; r < rows; r += STEP_THREADS) {
-    const T* k = r < np ? a.k_pre + po + (int64_t)r * D : kc + (int64_t)(r - np) * D;
-    float x = 0.f;
-    for (int p = 0; p < D / E; ++p) {
-      float f[E];
-      Piece<T>::unpack(ld16(k + p * E), f);
+  bf16x8 qhi[sizeof(T) == 2 ? KS : 1], qlo[sizeof(T) == 2 ? KS : 1];
+  float qf[sizeof(T) == 2 ? 1 : D / 2];
+  f32x16 o[DB];
+  float M, l;
+
+  // the lane's query, row `q` of D floats in LDS
+  __device__ __forceinline__ void take_query(const float* q, int h) {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) x = fmaf(f[e], qs[p * E + e], x);
+      for (int kk = 0; kk < KS; ++kk) {
+        u32x4 wh, wl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x0 = q[16 * kk + 8 * h + 2 * i], x1 = q[16 * kk + 8 * h + 2 * i + 1];
+          wh[i] = pack_bf16x2(x0, x1);
+          wl[i] = pack_bf16x2(x0 - bf16_lo(wh[i]), x1 - bf16_hi(wh[i]));
+        }
+        qhi[kk] = __builtin_bit_cast(bf16x8, wh);
+        qlo[kk] = __builtin_bit_cast(bf16x8, wl);
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < D / 8; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qf[4 * p + j] = q[8 * p + 4 * h + j];
     }
-    sc[r] = x;
-    m = fmaxf(m, x);
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[b][v] = 0.f;
+    M = -INFINITY;
+    l = 0.f;
   }
-  red[tid] = m;
-  __threadfence_block();
-  __syncthreads();
-  for (int i = 0; i < STEP_THREADS; ++i) m = fmaxf(m, red[i]);
-  __syncthreads();
-  float l = 0.f;
-  for (int r = tid; r < rows; r += STEP_THREADS) l += exp2f(sc[r] - m);
-  red[tid] = l;
-  __syncthreads();
-  l = 0.f;
-  for (int i = 0; i < STEP_THREADS; ++i) l += red[i];
-  const int wave = tid >> 6, lane = tid & 63;
-  float v0 = 0.f, v1 = 0.f;
-  for (int r = wave; r < rows; r += STEP_THREADS / 64) {
-    const T* v = r < np ? a.v_pre + po + (int64_t)r * D : vc + (int64_t)(r - np) * D;
-    const float p = exp2f(sc[r] - m);
-    v0 = fmaf(p, val(v, lane), v0);
-    if (lane + 64 < D) v1 = fmaf(p, val(v, lane + 64), v1);
+
+  // Rows r .. r + 31 of a slice (those past `last` read row `last`).  bf16:
+  // pieces 16 kk + 8 h of the lane's row l % 32 of both.  fp32: pieces 2p + h
+  // of the key row; of the values what the A operands of 32x32x2 take, element
+  // 32 b + l % 32 of row 8a + 4h + c.
+  __device__ __forceinline__ static void load(Rows& x, const T* kb, const T* vb, int r, int last,
+                                              int lane) {
+    const int h = lane >> 5;
+    const int64_t row = min(r + (lane & 31), last);
+    if constexpr (sizeof(T) == 2) {
+      const T* kp = kb + row * D + 8 * h;
+      const T* vp = vb + row * D + 8 * h;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) x.k[kk] = ld16(kp + 16 * kk);
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const u32x4 w = ld16(vp + 16 * kk);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.v[4 * kk + i] = w[i];
+      }
+    } else {
+      const T* kp = kb + row * D + 4 * h;
+#pragma unroll
+      for (int p = 0; p < D / 8; ++p) x.k[p] = ld16(kp + 8 * p);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const T* vp = vb + (int64_t)min(r + 8 * (v / 4) + 4 * h + v % 4, last) * D;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)  // (elements past the head size are never stored)
+          x.v[v * DB + b] = __float_as_uint(vp[min(32 * b + (lane & 31), D - 1)]);
+      }
+    }
   }
-  acc[wave][lane] = v0;
-  if (lane + 64 < D) acc[wave][lane + 64] = v1;
-  if (a.w_out)
-    for (int r = tid; r < rows; r += STEP_THREADS)
-      a.w_out[wo + r] = (a.w_in && r < n ? a.w_in[wo + r] : 0.f) + exp2f(sc[r] - m) / l;
+
+  // one block of rows r .. r + 31, of which those before r1 count; vt is the
+  // wave's own value tile in LDS
+  __device__ __forceinline__ void step(const Rows& x, int r, int r1, float c, char* vt, int lane) {
+    const int h = lane >> 5;
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.f;
+    if constexpr (sizeof(T) == 2) {
+      // the values go to LDS row by row while the scores are multiplied (the
+      // wave's own tile, and LDS serves a wave in order: no barrier)
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const u32x4 w = {x.v[4 * kk], x.v[4 * kk + 1], x.v[4 * kk + 2], x.v[4 * kk + 3]};
+        st16(vt + (lane & 31) * PITCH + 32 * kk + 16 * h, w);
+      }
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const bf16x8 k = __builtin_bit_cast(bf16x8, x.k[kk]);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qhi[kk], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qlo[kk], s, 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < D / 8; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.k[p][j]), qf[4 * p + j], s, 0, 0, 0);
+    }
+    float mb = -INFINITY;
+    if (r + PRE_ROWS <= r1) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[v] *= c;
+        mb = fmaxf(mb, s[v]);
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[v] = r + 8 * (v / 4) + 4 * h + v % 4 < r1 ? s[v] * c : -INFINITY;
+        mb = fmaxf(mb, s[v]);
+      }
+    }
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb), __float_as_uint(mb), false, false);
+    mb = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    // finite in every lane from the first block on (its first row counts)
+    if (__any(mb > M + PRE_RESCALE)) {
+      const float mn = fmaxf(M, mb);
+      const float f = fast_exp2(M - mn);  // 0 while M = -inf
+      M = mn;
+      l *= f;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[b][v] *= f;
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        u32x4 p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[i] = pack_bf16x2(fast_exp2(s[8 * t + 2 * i] - M), fast_exp2(s[8 * t + 2 * i + 1] - M));
+          l += bf16_lo(p[i]) + bf16_hi(p[i]);
+        }
+        const bf16x8 pb = __builtin_bit_cast(bf16x8, p);
+        // V^T: elements 32 b + 16 (l/16 % 2) .. of rows 16 t + 8 j + 4 h + 0..3
+        const int i16 = lane & 15;
+        const char* at = vt + (16 * t + 4 * h + i16 / 4) * PITCH + 32 * ((lane >> 4) & 1) + 8 * (i16 % 4);
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+          const s16x4 lo = lds_read_tr16(at + 64 * b), hi = lds_read_tr16(at + 64 * b + 8 * PITCH);
+          const s16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pb, o[b], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float p = fast_exp2(s[v] - M);
+        l += p;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+          o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.v[v * DB + b]), p, o[b], 0, 0, 0);
+      }
+    }
+  }
+
+  // joins another wave's state of the same queries (LDS, [register][lane])
+  __device__ __forceinline__ void put(float* at, int lane) const {
+    at[lane] = M;
+    at[64 + lane] = l;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) at[(2 + 16 * b + v) * 64 + lane] = o[b][v];
+  }
+  __device__ __forceinline__ void join(const float* at, int lane) {
+    const float m2 = at[lane], mn = fmaxf(M, m2);
+    const float f = M == -INFINITY ? 0.f : fast_exp2(M - mn);
+    const float g = m2 == -INFINITY ? 0.f : fast_exp2(m2 - mn);
+    M = mn;
+    l = l * f + at[64 + lane] * g;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[b][v] = o[b][v] * f + at[(2 + 16 * b + v) * 64 + lane] * g;
+  }
+  static constexpr int STATE_BYTES = (2 + 16 * DB) * 64 * 4;
+};
+
+// one workgroup per (prefix, head, chunk of rows, NQ tiles of queries):
+// PRE_KEY_WAVES waves a tile
+template <typename T, int D, int NQ>
+__global__ __launch_bounds__(64 * PRE_KEY_WAVES * NQ, sizeof(T) == 2 ? 2 : 1) void prefix_kernel(
+    const T* __restrict__ q, const T* __restrict__ k_pre, const T* __restrict__ v_pre,
+    const int32_t* __restrict__ pre_len, const int32_t* __restrict__ cur_tok,
+    const int32_t* __restrict__ pos, int32_t L_meta, int32_t H, int32_t P_cap, int32_t per,
+    int32_t n_chunk, int32_t n_slice, float c, int rotate, PrefixFreq tab, float* __restrict__ part_o,
+    float2* __restrict__ part_ml) {
+  using Tile = PrefixTile<T, D>;
+  constexpr int THREADS = 64 * PRE_KEY_WAVES * NQ;
+  constexpr int HD = D / 2;
+  constexpr int QPITCH = D + 4;
+  constexpr int Q_BYTES = PRE_QUERIES * QPITCH * 4;
+  constexpr int TILE_BYTES = PRE_KEY_WAVES * Tile::V_BYTES;
+  constexpr int JOIN_BYTES = PRE_KEY_WAVES / 2 * Tile::STATE_BYTES;
+  constexpr int PER_TILE = std::max(std::max(Q_BYTES, TILE_BYTES), JOIN_BYTES);
+  __shared__ __align__(16) char lds[NQ * PER_TILE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tile = wave / PRE_KEY_WAVES, kw = wave % PRE_KEY_WAVES;
+  // chunks of a slice and slices first, tiles of queries behind: workgroups
+  // that read the same rows are a multiple of the slices' chunks apart
+  const int qt = blockIdx.x / (n_slice * n_chunk);
+  const int rest = blockIdx.x - qt * (n_slice * n_chunk);
+  const int slice = rest / n_chunk, chunk = rest - slice * n_chunk;
+  const int g = slice / H, h_ = slice - g * H;
+  const int q0 = qt * NQ * PRE_QUERIES;  // first query of the workgroup (of the prefix's `per`)
+
+  const int n = min(max(pre_len[g], 0), P_cap);
+  const int each = ((n + n_chunk - 1) / n_chunk + PRE_ROWS - 1) / PRE_ROWS * PRE_ROWS;
+  const int r0 = min(chunk * (int64_t)each, (int64_t)n), r1 = min((int64_t)r0 + each, (int64_t)n);
+  const int64_t at = ((int64_t)g * H + h_) * P_cap * D;
+  const T* kb = k_pre + at;
+  const T* vb = v_pre + at;
+  typename Tile::Rows A, B;
+  constexpr int STRIDE = PRE_ROWS * PRE_KEY_WAVES;
+  int r = r0 + PRE_ROWS * kw;
+  if (r < r1) Tile::load(A, kb, vb, r, r1 - 1, lane);
+
+  // the tile's queries, rotated, as floats in LDS
+  for (int i = tid; i < NQ * PRE_QUERIES * HD; i += THREADS) {
+    const int j = i / HD, e = i - j * HD;
+    const int s = g * per + q0 + j;
+    float x = 0.f, y = 0.f;
+    if (q0 + j < per) {
+      const T* src = q + ((int64_t)s * H + h_) * D;
+      if constexpr (sizeof(T) == 2) {
+        x = bf16_lo((uint32_t)src[e]);
+        y = bf16_lo((uint32_t)src[e + HD]);
+      } else {
+        x = src[e];
+        y = src[e + HD];
+      }
+      if (rotate) {
+        const int t = cur_tok[s];
+        // (a token outside the metadata: its step's output does not come from here)
+        const double ps = t >= 0 && t < L_meta ? (double)pos[(int64_t)s * L_meta + t] : 0.0;
+        const double two_pi = 6.283185307179586476925286766559;
+        const double inv_two_pi = 0.15915494309189533576888376337251;
+        double ang = ps * tab.w[e];
+        ang -= two_pi * rint(ang * inv_two_pi);
+        float sn, cs;
+        sincosf((float)ang, &sn, &cs);
+        const float x1 = x;
+        x = x1 * cs - y * sn;
+        y = y * cs + x1 * sn;
+      }
+    }
+    float* dst = reinterpret_cast<float*>(lds + j / PRE_QUERIES * PER_TILE) + j % PRE_QUERIES * QPITCH;
+    dst[e] = x;
+    dst[e + HD] = y;
+  }
   __syncthreads();
-  if (tid < D) {
-    float x = 0.f;
-    for (int w = 0; w < STEP_THREADS / 64; ++w) x += acc[w][tid];
-    x /= l;
-    if constexpr (sizeof(T) == 2) o[tid] = f32_to_bf16(x);
-    else o[tid] = x;
+  char* mine = lds + tile * PER_TILE;
+  Tile st;
+  st.take_query(reinterpret_cast<const float*>(mine) + (lane & 31) * QPITCH, lane >> 5);
+  __syncthreads();  // every wave has its queries; the tiles of values take their place
+
+  char* vt = mine + kw * Tile::V_BYTES;
+  for (; r + 2 * STRIDE < r1; r += 2 * STRIDE) {
+    Tile::load(B, kb, vb, r + STRIDE, r1 - 1, lane);
+    st.step(A, r, r1, c, vt, lane);
+    Tile::load(A, kb, vb, r + 2 * STRIDE, r1 - 1, lane);
+    st.step(B, r + STRIDE, r1, c, vt, lane);
+  }
+  if (r < r1) {
+    const bool more = r + STRIDE < r1;
+    if (more) Tile::load(B, kb, vb, r + STRIDE, r1 - 1, lane);
+    st.step(A, r, r1, c, vt, lane);
+    if (more) st.step(B, r + STRIDE, r1, c, vt, lane);
+  }
+
+  // both halves of the wave hold a part of each query's sum
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.l), __float_as_uint(st.l), false, false);
+  st.l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  // the key waves' states meet pairwise in LDS
+  float* slots = reinterpret_cast<float*>(mine);
+  constexpr int SLOT = Tile::STATE_BYTES / 4;
+  __syncthreads();
+  if (kw >= 2) st.put(slots + (kw - 2) * SLOT, lane);
+  __syncthreads();
+  if (kw < 2) st.join(slots + kw * SLOT, lane);
+  __syncthreads();
+  if (kw == 1) st.put(slots, lane);
+  __syncthreads();
+  if (kw == 0) {
+    st.join(slots, lane);
+    const int j = q0 + tile * PRE_QUERIES + (lane & 31);
+    if (j < per) {
+      const int64_t p = (((int64_t)(g * per + j)) * H + h_) * n_chunk + chunk;
+      if (lane < 32) part_ml[p] = make_float2(st.M, st.l);
+#pragma unroll
+      for (int b = 0; b < Tile::DB; ++b)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int e = 32 * b + 8 * a + 4 * (lane >> 5);
+          if (e < D) {
+            const f32x4 w = {st.o[b][4 * a], st.o[b][4 * a + 1], st.o[b][4 * a + 2], st.o[b][4 * a + 3]};
+            *reinterpret_cast<f32x4*>(part_o + p * D + e) = w;
+          }
+        }
+    }
   }
 }
 
-static int step_checks(const std::string& w, const void* q, const void* k_new, const void* v_new,
-                       const void* k_cache, const void* v_cache, const int32_t* kv_len,
-                       const int32_t* cur_tok, const int32_t* vu, const int32_t* pos,
-                       int32_t L_meta, const void* o, int32_t b, int32_t H, int32_t L_cap,
-                       int32_t d_head, sckv_dtype dt, float scale, float rope_theta,
-                       const void* ws) {
-  if (!q || !k_new || !v_new || !k_cache || !v_cache || !kv_len || !cur_tok || !vu || !o || !ws)
-    return fail(SCKV_EINVAL, w + ": null pointer");
-  if (!valid_dtype(dt)) return fail(SCKV_EINVAL, w + ": unknown dtype");
-  if (!supported_d(d_head)) return fail(SCKV_EUNSUP, w + ": d_head must be 64 or 80");
-  if (b <= 0 || H <= 0 || L_cap <= 0 || L_meta <= 0)
-    return fail(SCKV_EINVAL, w + ": sizes must be positive");
-  if ((int64_t)b * H > 0x7fffffff) return fail(SCKV_EUNSUP, w + ": too many slices");
-  if (!(scale > 0.f) || std::isinf(scale)) return fail(SCKV_EINVAL, w + ": scale must be finite and > 0");
-  if (!(rope_theta >= 0.f) || std::isinf(rope_theta))
-    return fail(SCKV_EINVAL, w + ": rope_theta must be finite and >= 0");
-  if (rope_theta > 0.f && !pos) return fail(SCKV_EINVAL, w + ": null pos");
-  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) ||
-      !aligned16(v_cache) || !aligned16(o) || !aligned16(ws))
-    return fail(SCKV_EINVAL, w + ": buffers must be 16-byte aligned");
-  return SCKV_OK;
+// Chunks of each prefix slice: as many as give every CU its workgroups (two
+// of one tile, one of two tiles: about 220 registers a thread), none of less
+// than 128 rows.
+constexpr int PRE_FILL_WAVES = 2048;
+static int prefix_tiles(bool bf16, int32_t per) { return bf16 && per > PRE_QUERIES ? 2 : 1; }
+int prefix_chunks(bool bf16, int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap) {
+  const int nq = prefix_tiles(bf16, per);
+  const int64_t wgs = (int64_t)n_prefix * H * ((per + nq * PRE_QUERIES - 1) / (nq * PRE_QUERIES));
+  const int64_t want = std::max<int64_t>(1, PRE_FILL_WAVES / (PRE_KEY_WAVES * nq) / wgs);
+  return (int)std::min<int64_t>(want, (P_cap + 127) / 128);
 }
 
 template <typename T, int D>
-static int launch_step(const void* q, const void* k_new, const void* v_new, const void* k_pre,
-                       const void* v_pre, const int32_t* pre_len, int32_t per, int32_t P_cap,
-                       void* k_cache, void* v_cache, const int32_t* kv_len,
-                       const int32_t* cur_tok, const int32_t* vu, const int32_t* pos,
-                       int32_t L_meta, void* o, const float* w_in, float* w_out, int32_t b,
-                       int32_t H, int32_t L_cap, float scale, float theta, void* ws,
-                       int32_t* status, const char* what, hipStream_t stream) {
-  StepFreq tab;
+static int launch_prefix_typed(const void* q, const void* k, const void* v, const int32_t* len,
+                               int32_t n_prefix, int32_t P_cap, const int32_t* cur_tok,
+                               const int32_t* pos, int32_t L_meta, int32_t b, int32_t H,
+                               float scale, float theta, float* part_o, float* part_ml,
+                               hipStream_t stream) {
+  const int per = b / n_prefix;
+  const int nq = prefix_tiles(sizeof(T) == 2, per);
+  const int qtiles = (per + nq * PRE_QUERIES - 1) / (nq * PRE_QUERIES);
+  const int nc = prefix_chunks(sizeof(T) == 2, n_prefix, H, per, P_cap);
+  const int64_t wgs = (int64_t)n_prefix * H * nc * qtiles;
+  if (wgs > 0x7fffffff) return fail(SCKV_EUNSUP, "shared_prefix_decode_attn: too many slices");
+  PrefixFreq tab;
   for (int i = 0; i < 40; ++i) tab.w[i] = 0.0;
   if (theta > 0.f)
     for (int i = 0; i < D / 2; ++i) tab.w[i] = std::pow((double)theta, -2.0 * i / D);
-  StepArgs<T> a = {(const T*)q, (const T*)k_new, (const T*)v_new, (const T*)k_pre, (const T*)v_pre,
-                   (T*)k_cache, (T*)v_cache, (T*)o, pre_len, kv_len, cur_tok, vu, pos, w_in, w_out,
-                   (float*)ws, status, per, P_cap, L_meta, H, L_cap, theta > 0.f ? 1 : 0,
-                   scale * 1.4426950408889634f};
-  step_kernel<T, D><<<b * H, STEP_THREADS, 0, stream>>>(a, tab);
-  return hip_check(hipGetLastError(), what);
+  auto go = [&](auto kernel, int threads) {
+    kernel<<<(unsigned)wgs, threads, 0, stream>>>(
+        static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), len, cur_tok,
+        pos, L_meta, H, P_cap, per, nc, n_prefix * H, scale * 1.4426950408889634f, theta > 0.f, tab,
+        part_o, reinterpret_cast<float2*>(part_ml));
+    return hip_check(hipGetLastError(), "shared_prefix_decode_attn: prefix launch");
+  };
+  if constexpr (sizeof(T) == 2)
+    if (nq == 2) return go(prefix_kernel<T, D, 2>, 128 * PRE_KEY_WAVES);
+  return go(prefix_kernel<T, D, 1>, 64 * PRE_KEY_WAVES);
+}
+
+int launch_prefix(const void* q, const void* k, const void* v, const int32_t* len,
+                  int32_t n_prefix, int32_t P_cap, const int32_t* cur_tok, const int32_t* pos,
+                  int32_t L_meta, int32_t b, int32_t H, int32_t d_head, sckv_dtype dt, float scale,
+                  float theta, float* part_o, float* part_ml, hipStream_t stream) {
+#define SCKV_PREFIX(T, D)                                                                          \
+  launch_prefix_typed<T, D>(q, k, v, len, n_prefix, P_cap, cur_tok, pos, L_meta, b, H, scale,      \
+                            theta, part_o, part_ml, stream)
+  if (dt == SCKV_BF16) return d_head == 64 ? SCKV_PREFIX(uint16_t, 64) : SCKV_PREFIX(uint16_t, 80);
+  return d_head == 64 ? SCKV_PREFIX(float, 64) : SCKV_PREFIX(float, 80);
+#undef SCKV_PREFIX
 }
 
 }  // namespace sckv
-
-using namespace sckv;
-
-#define SCKV_STEP(T, D, KP, VP, PL, PER, PC, WI, WO, WHAT)                                         \
-  launch_step<T, D>(q, k_new, v_new, KP, VP, PL, PER, PC, k_cache, v_cache, kv_len, cur_tok, vu,  \
-                    pos, L_meta, o, WI, WO, b, H, L_cap, scale, rope_theta, ws, status, WHAT, stream)
-
-extern "C" size_t sckv_decode_weights_workspace_bytes(int32_t b, int32_t H, int32_t L_cap,
-                                                      int32_t d_head) {
-  if (b <= 0 || H <= 0 || L_cap <= 0 || d_head <= 0) return 0;
-  return (size_t)b * H * L_cap * sizeof(float);
-}
-
-extern "C" int compacted_decode_attn_weights(
-    const void* q, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
-    const int32_t* kv_len, const int32_t* cur_tok, const int32_t* vu, const int32_t* pos,
-    int32_t L_meta, void* o, const float* w_in, float* w_out, int32_t b, int32_t H, int32_t L_cap,
-    int32_t d_head, sckv_dtype dt, float scale, float rope_theta, void* ws, size_t ws_bytes,
-    int32_t* status, hipStream_t stream) {
-  clear_error();
-  const char* W = "compacted_decode_attn_weights";
-  const int rc = step_checks(W, q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos, L_meta,
-                             o, b, H, L_cap, d_head, dt, scale, rope_theta, ws);
-  if (rc) return rc;
-  if (!w_out) return fail(SCKV_EINVAL, std::string(W) + ": null pointer");
-  if (!aligned4(w_out) || !aligned4(w_in))
-    return fail(SCKV_EINVAL, std::string(W) + ": w_in and w_out must be 4-byte aligned");
-  if (ws_bytes < sckv_decode_weights_workspace_bytes(b, H, L_cap, d_head))
-    return fail(SCKV_EINVAL, std::string(W) + ": workspace too small");
-  if (dt == SCKV_BF16)
-    return d_head == 64 ? SCKV_STEP(uint16_t, 64, nullptr, nullptr, nullptr, 1, 0, w_in, w_out, W)
-                        : SCKV_STEP(uint16_t, 80, nullptr, nullptr, nullptr, 1, 0, w_in, w_out, W);
-  return d_head == 64 ? SCKV_STEP(float, 64, nullptr, nullptr, nullptr, 1, 0, w_in, w_out, W)
-                      : SCKV_STEP(float, 80, nullptr, nullptr, nullptr, 1, 0, w_in, w_out, W);
-}
-
-extern "C" size_t sckv_shared_decode_workspace_bytes(int32_t b, int32_t H, int32_t n_prefix,
-                                                     int32_t P_cap, int32_t L_cap,
-                                                     int32_t d_head) {
-  if (b <= 0 || H <= 0 || n_prefix <= 0 || P_cap <= 0 || L_cap <= 0 || d_head <= 0) return 0;
-  return (size_t)b * H * ((size_t)P_cap + L_cap) * sizeof(float);
-}
-
-extern "C" int shared_prefix_decode_attn(
-    const void* q, const void* k_new, const void* v_new, const void* k_prefix,
-    const void* v_prefix, const int32_t* prefix_len, int32_t n_prefix, int32_t P_cap,
-    void* k_cache, void* v_cache, const int32_t* kv_len, const int32_t* cur_tok,
-    const int32_t* vu, const int32_t* pos, int32_t L_meta, void* o, int32_t b, int32_t H,
-    int32_t L_cap, int32_t d_head, sckv_dtype dt, float scale, float rope_theta, void* ws,
-    size_t ws_bytes, int32_t* status, hipStream_t stream) {
-  clear_error();
-  const char* W = "shared_prefix_decode_attn";
-  const int rc = step_checks(W, q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos, L_meta,
-                             o, b, H, L_cap, d_head, dt, scale, rope_theta, ws);
-  if (rc) return rc;
-  if (!k_prefix || !v_prefix || !prefix_len) return fail(SCKV_EINVAL, std::string(W) + ": null pointer");
-  if (n_prefix <= 0 || P_cap <= 0 || b % n_prefix)
-    return fail(SCKV_EINVAL, std::string(W) + ": b must be a multiple of n_prefix, sizes positive");
-  if (!aligned16(k_prefix) || !aligned16(v_prefix))
-    return fail(SCKV_EINVAL, std::string(W) + ": buffers must be 16-byte aligned");
-  if (ws_bytes < sckv_shared_decode_workspace_bytes(b, H, n_prefix, P_cap, L_cap, d_head))
-    return fail(SCKV_EINVAL, std::string(W) + ": workspace too small");
-  const int per = b / n_prefix;
-  if (dt == SCKV_BF16)
-    return d_head == 64 ? SCKV_STEP(uint16_t, 64, k_prefix, v_prefix, prefix_len, per, P_cap, nullptr, nullptr, W)
-                        : SCKV_STEP(uint16_t, 80, k_prefix, v_prefix, prefix_len, per, P_cap, nullptr, nullptr, W);
-  return d_head == 64 ? SCKV_STEP(float, 64, k_prefix, v_prefix, prefix_len, per, P_cap, nullptr, nullptr, W)
-                      : SCKV_STEP(float, 80, k_prefix, v_prefix, prefix_len, per, P_cap, nullptr, nullptr, W);
-}
