@@ -567,53 +567,6 @@ __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
 // rows are in flight while a block is computed.
 constexpr float DM_RESCALE = 8.f;
 
-// Sums v[0..NV) over the 32 lanes of each half-wave.  While NV is even a
-// step halves the values a lane keeps (the lane whose MASK bit is set keeps
-// the upper half); odd counts finish with plain butterflies.  On return the
-// lane holds the sums of values [base, base + count).  Lanes exchange by
-// register moves (row swap, DPP), not through LDS: of the 16-lane rows' moves
-// the half-row mirror stands in for an exchange of lanes 4 apart (its partner
-// differs in the MASK bit, and the two steps after it cover the rest).
-template <int MASK>
-__device__ __forceinline__ float partner(float x) {
-  static_assert(MASK == 8 || MASK == 4 || MASK == 2 || MASK == 1, "within a row of 16 lanes");
-  return dpp_mov<MASK == 8 ? DPP_ROW_ROR8 : MASK == 4 ? DPP_ROW_HALF_MIRROR
-                 : MASK == 2 ? DPP_QUAD_XOR2 : DPP_QUAD_XOR1>(x);
-}
-template <int NV, int MASK>
-__device__ __forceinline__ void half_wave_reduce(float* v, int lane, int& base) {
-  if constexpr (MASK > 0) {
-    if constexpr (NV % 2 == 0) {
-      constexpr int HV = NV / 2;
-      const bool up = (lane & MASK) != 0;
-#pragma unroll
-      for (int j = 0; j < HV; ++j) {
-        if constexpr (MASK == 16) {
-          float a = v[j], b = v[j + HV];
-          swap_rows16(a, b);  // even rows: their and their partner's v[j]; odd rows: v[j + HV]
-          v[j] = a + b;
-        } else {
-          const float send = up ? v[j] : v[j + HV];
-          const float keep = up ? v[j + HV] : v[j];
-          v[j] = keep + partner<MASK>(send);
-        }
-      }
-      if (up) base += HV;
-      half_wave_reduce<HV, MASK / 2>(v, lane, base);
-    } else {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) v[j] += partner<MASK>(v[j]);
-      half_wave_reduce<NV, MASK / 2>(v, lane, base);
-    }
-  }
-}
-template <int NV, int MASK>
-constexpr int half_wave_count() {
-  if constexpr (MASK == 0) return NV;
-  else if constexpr (NV % 2 == 0) return half_wave_count<NV / 2, MASK / 2>();
-  else return half_wave_count<NV, MASK / 2>();
-}
-
 template <int D, int NW, bool FINAL, bool SPEC2, typename X>
 __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k_new,

@@ -75,6 +75,10 @@ CASES = [
     (1, 2, 64, "bf16", 1025, 1025, False, 0.4),
     (2, 1, 80, "f32", 700, 65, True, 0.5),
     (1, 1, 64, "bf16", 3000, 129, True, 0.1),
+    (4, 64, 64, "bf16", 530, 530, False, 0.5),    # two tiles of queries and of rows a wave
+    (4, 64, 80, "bf16", 300, 131, True, 0.4),
+    (40, 13, 64, "bf16", 520, 5, False, 0.3),     # two tiles of rows, one of queries
+    (3, 100, 80, "f32", 260, 45, False, 0.5),
 ]
 
 
