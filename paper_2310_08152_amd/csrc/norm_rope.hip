@@ -8,7 +8,7 @@
 // piece of a row's first half and the matching piece of its second half, so
 // both elements of a rotated pair are in one thread; the LANES threads of a
 // row are neighbours and add up their squares by register moves.  The pair's
-// angles are taken once and serve q and k of the HPT heads of the thread.
+// angles are taken once and serve the HPT heads of the thread.
 #include <cmath>
 
 #include "sckv_common.h"
@@ -21,10 +21,12 @@ struct NormFreq {
 
 template <typename T>
 struct NormArgs {
-  const T *q, *k, *v;
-  T *q_out, *k_out, *v_out;
-  const T *q_weight, *k_weight;
-  int64_t xb, xh, xr, q_out_s, kv_s;
+  const T* x[3];  // those of q, k and v that are given, in this order
+  T* y[3];
+  const T* weight[3];
+  int64_t y_stride[3];
+  int32_t kind[3];  // 0 q, 1 k, 2 v
+  int64_t xb, xh, xr;
   const int32_t *pos, *cur_tok, *row0;
   int32_t* status;
   float eps;
@@ -51,8 +53,19 @@ __device__ __forceinline__ float row_sum(float x, int lane) {
 }
 
 constexpr int NORM_THREADS = 256;
+constexpr int NORM_SMALL = 2048;   // waves (a head a thread) that fill the SIMDs twice
+constexpr int NORM_LARGE = 32768;  // 32 a SIMD
 
-template <typename T, int D, int HPT>
+// Shapes, measured on token-major bf16 inputs, 32 heads of 80, us:
+//   NZ = 3, HPT = 4 (a thread takes its heads' q, k and v): large launches,
+//     16 x 4096 tokens 428 (4.7 TB/s) against 449 with a tensor a workgroup;
+//     8 x 1024 47 against 44.
+//   NZ = 1 (blockIdx.y picks the tensor), HPT = 4: from NORM_SMALL waves on;
+//     HPT = 1 gives 70 at 8 x 1024, its angles taken for one row each.
+//   NZ = 1, HPT = 1: the fewest rows a thread, one token's step 4.1 against 5.6.
+// fp32 pieces hold 4 elements, so angles weigh half: NZ = 3 with HPT = 2 (16 x
+// 1024 tokens 195, with a tensor a workgroup 204).
+template <typename T, int D, int HPT, int NZ>
 __global__ __launch_bounds__(NORM_THREADS) void norm_rope_kernel(NormArgs<T> a, NormFreq tab) {
   constexpr int E = Piece<T>::E;
   constexpr int HALF = D / 2;
@@ -69,17 +82,64 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_rope_kernel(NormArgs<T> a, 
   const int s = fast_div(sg, a.by_hg);
   const int h0 = (sg - s * a.n_hg) * HPT;
 
-  // the row's token, its position, and where its key and value go
+  // the tensors of this thread (all three, or one), their pieces and weights;
+  // offsets are shared by those that share strides
+  int kind[NZ];
+  const T* from[NZ];
+  u32x4 lo[NZ], hi[NZ], lo1[NZ], hi1[NZ], wlo[NZ], whi[NZ];
+  bool weighed[NZ];
+  int64_t xo = s * a.xb + h0 * a.xh + t * a.xr + p * E;
+#pragma unroll
+  for (int z = 0; z < NZ; ++z) {
+    const int i = NZ == 1 ? (int)blockIdx.y : z;
+    kind[z] = NZ == 3 ? z : i == 0 ? a.kind[0] : i == 1 ? a.kind[1] : a.kind[2];
+    from[z] = i == 0 ? a.x[0] : i == 1 ? a.x[1] : a.x[2];
+    lo[z] = hi[z] = lo1[z] = hi1[z] = wlo[z] = whi[z] = u32x4{0, 0, 0, 0};
+    if (live) {
+      lo[z] = ld16(from[z] + xo);
+      hi[z] = ld16(from[z] + xo + HALF);
+    }
+    const T* w = i == 0 ? a.weight[0] : i == 1 ? a.weight[1] : a.weight[2];
+    weighed[z] = w != nullptr;
+    if (weighed[z]) {
+      wlo[z] = ld16(w + p * E);
+      whi[z] = ld16(w + HALF + p * E);
+    }
+  }
+  // the row's token, its position, and where it goes
   const int64_t tok = (int64_t)(a.cur_tok ? a.cur_tok[s] : a.tok0) + t;
   const bool tok_ok = !a.cur_tok || (tok >= 0 && tok < a.L_meta);
   const int r0 = a.row0 ? a.row0[s] : 0;
-  const bool kv_ok = r0 >= 0 && (int64_t)r0 + a.n <= a.kv_rows;
+  const bool room = r0 >= 0 && (int64_t)r0 + a.n <= a.kv_rows;
+  bool turns = false, caches = false;
+  T* to[NZ];
+  int64_t ys[NZ], yo[NZ];  // (k and v: the same stride and offset)
+#pragma unroll
+  for (int z = 0; z < NZ; ++z) {
+    const int i = NZ == 1 ? (int)blockIdx.y : z;
+    turns = turns || kind[z] < 2;
+    caches = caches || kind[z] > 0;
+    to[z] = i == 0 ? a.y[0] : i == 1 ? a.y[1] : a.y[2];
+    if (z == 2) {
+      ys[z] = ys[1];
+      yo[z] = yo[1];
+    } else {
+      ys[z] = i == 0 ? a.y_stride[0] : i == 1 ? a.y_stride[1] : a.y_stride[2];
+      yo[z] = ((int64_t)s * a.H + h0) * ys[z] + ((int64_t)(kind[z] > 0 ? r0 : 0) + t) * D + p * E;
+    }
+  }
   if (live && h0 == 0 && p == 0 && a.status) {
-    if (!tok_ok) atomicOr(a.status, SCKV_STATUS_TOKEN);
-    if (!kv_ok && t == 0 && (a.k || a.v)) atomicOr(a.status, SCKV_STATUS_CAP);
+    if (turns && !tok_ok) atomicOr(a.status, SCKV_STATUS_TOKEN);
+    if (caches && !room && t == 0) atomicOr(a.status, SCKV_STATUS_CAP);
   }
   float cs[E], sn[E];
-  if (a.rotate) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    cs[e] = 1.f;
+    sn[e] = 0.f;
+  }
+  const bool turned = turns && a.rotate;
+  if (turned) {
     const double two_pi = 6.283185307179586476925286766559;
     const double inv_two_pi = 0.15915494309189533576888376337251;
     const double ps = tok_ok ? (double)a.pos[(int64_t)s * a.L_meta + tok] : 0.0;
@@ -93,83 +153,70 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_rope_kernel(NormArgs<T> a, 
       cs[e] = co;
     }
   }
-  const int64_t xo = s * a.xb + t * a.xr + p * E;
-  const int64_t qo = (int64_t)s * a.H * a.q_out_s + (int64_t)t * D + p * E;
-  const int64_t ko = (int64_t)s * a.H * a.kv_s + ((int64_t)r0 + t) * D + p * E;
-
-  auto turn = [&](u32x4& lo, u32x4& hi, const float* wl, const float* wh) {
-    float x1[E], x2[E], sq = 0.f;
-    Piece<T>::unpack(lo, x1);
-    Piece<T>::unpack(hi, x2);
-#pragma unroll
-    for (int e = 0; e < E; ++e) sq = fmaf(x2[e], x2[e], fmaf(x1[e], x1[e], sq));
-    const float rms = 1.f / sqrtf(row_sum<LANES>(sq, lane) * (1.f / D) + a.eps);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      x1[e] *= rms * wl[e];
-      x2[e] *= rms * wh[e];
-    }
-    if (a.rotate) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float y1 = fmaf(x1[e], cs[e], -(x2[e] * sn[e]));
-        x2[e] = fmaf(x2[e], cs[e], x1[e] * sn[e]);
-        x1[e] = y1;
-      }
-    }
-    if (!tok_ok) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) x1[e] = x2[e] = __builtin_nanf("");
-    }
-    lo = Piece<T>::pack(x1);
-    hi = Piece<T>::pack(x2);
-  };
-  float qwl[E], qwh[E], kwl[E], kwh[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) qwl[e] = qwh[e] = kwl[e] = kwh[e] = 1.f;
-  if (a.q_weight) {
-    Piece<T>::unpack(ld16(a.q_weight + p * E), qwl);
-    Piece<T>::unpack(ld16(a.q_weight + HALF + p * E), qwh);
-  }
-  if (a.k_weight) {
-    Piece<T>::unpack(ld16(a.k_weight + p * E), kwl);
-    Piece<T>::unpack(ld16(a.k_weight + HALF + p * E), kwh);
-  }
-  const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < HPT; ++i) {
-    const int h = h0 + i;
-    const bool on = live && h < a.H;
-    const int64_t x = xo + h * a.xh;
-    u32x4 ql = zero, qh = zero, kl = zero, kh = zero, vl = zero, vh = zero;
-    if (on) {
-      if (a.q) { ql = ld16(a.q + x); qh = ld16(a.q + x + HALF); }
-      if (a.k) { kl = ld16(a.k + x); kh = ld16(a.k + x + HALF); }
-      if (a.v) { vl = ld16(a.v + x); vh = ld16(a.v + x + HALF); }
-    }
-    if (a.q) {
-      turn(ql, qh, qwl, qwh);
-      if (on) {
-        st16(a.q_out + qo + h * a.q_out_s, ql);
-        st16(a.q_out + qo + h * a.q_out_s + HALF, qh);
+    const bool on = live && h0 + i < a.H;
+    // the next head's pieces are in flight while this one is computed
+    if (i + 1 < HPT && live && h0 + i + 1 < a.H) {
+      xo += a.xh;
+#pragma unroll
+      for (int z = 0; z < NZ; ++z) {
+        lo1[z] = ld16(from[z] + xo);
+        hi1[z] = ld16(from[z] + xo + HALF);
       }
     }
-    if (a.k) {
-      turn(kl, kh, kwl, kwh);
-      if (on && kv_ok) {
-        st16(a.k_out + ko + h * a.kv_s, kl);
-        st16(a.k_out + ko + h * a.kv_s + HALF, kh);
+#pragma unroll
+    for (int z = 0; z < NZ; ++z) {
+      if (kind[z] < 2) {
+        float x1[E], x2[E], w1[E], w2[E], sq = 0.f;
+        Piece<T>::unpack(lo[z], x1);
+        Piece<T>::unpack(hi[z], x2);
+#pragma unroll
+        for (int e = 0; e < E; ++e) sq = fmaf(x2[e], x2[e], fmaf(x1[e], x1[e], sq));
+        const float rms = 1.f / sqrtf(row_sum<LANES>(sq, lane) * (1.f / D) + a.eps);
+        if (weighed[z]) {
+          Piece<T>::unpack(wlo[z], w1);
+          Piece<T>::unpack(whi[z], w2);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            x1[e] *= rms * w1[e];
+            x2[e] *= rms * w2[e];
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            x1[e] *= rms;
+            x2[e] *= rms;
+          }
+        }
+        if (turned) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float y1 = fmaf(x1[e], cs[e], -(x2[e] * sn[e]));
+            x2[e] = fmaf(x2[e], cs[e], x1[e] * sn[e]);
+            x1[e] = y1;
+          }
+        }
+        if (!tok_ok) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) x1[e] = x2[e] = __builtin_nanf("");
+        }
+        lo[z] = Piece<T>::pack(x1);
+        hi[z] = Piece<T>::pack(x2);
       }
-    }
-    if (a.v && on && kv_ok) {
-      st16(a.v_out + ko + h * a.kv_s, vl);
-      st16(a.v_out + ko + h * a.kv_s + HALF, vh);
+      if (on && (kind[z] == 0 || room)) {
+        st16(to[z] + yo[z], lo[z]);
+        st16(to[z] + yo[z] + HALF, hi[z]);
+      }
+      yo[z] += ys[z];
+      lo[z] = lo1[z];
+      hi[z] = hi1[z];
     }
   }
 }
 
-template <typename T, int D, int HPT>
-static int launch_norm(NormArgs<T> a, int32_t b, const NormFreq& tab, hipStream_t stream) {
+template <typename T, int D, int HPT, int NZ>
+static int launch_norm(NormArgs<T> a, int32_t b, int count, const NormFreq& tab, hipStream_t stream) {
   constexpr int RPB = NORM_THREADS / 64 * (64 / (D / 2 / Piece<T>::E));
   a.n_hg = (a.H + HPT - 1) / HPT;
   const int64_t rows = (int64_t)b * a.n_hg * a.n;
@@ -177,27 +224,23 @@ static int launch_norm(NormArgs<T> a, int32_t b, const NormFreq& tab, hipStream_
   a.rows = (int32_t)rows;
   a.by_n = make_div((uint32_t)a.n);
   a.by_hg = make_div((uint32_t)a.n_hg);
-  norm_rope_kernel<T, D, HPT><<<(unsigned)((rows + RPB - 1) / RPB), NORM_THREADS, 0, stream>>>(a, tab);
+  const dim3 grid((unsigned)((rows + RPB - 1) / RPB), NZ == 1 ? (unsigned)count : 1u);
+  norm_rope_kernel<T, D, HPT, NZ><<<grid, NORM_THREADS, 0, stream>>>(a, tab);
   return hip_check(hipGetLastError(), "qk_norm_rope: launch");
 }
 
 template <typename T, int D>
-static int norm_typed(NormArgs<T> a, const void* q, const void* k, const void* v, void* q_out,
-                      void* k_out, void* v_out, const void* q_weight, const void* k_weight,
-                      int32_t b, float theta, hipStream_t stream) {
-  a.q = static_cast<const T*>(q);
-  a.k = static_cast<const T*>(k);
-  a.v = static_cast<const T*>(v);
-  a.q_out = static_cast<T*>(q_out);
-  a.k_out = static_cast<T*>(k_out);
-  a.v_out = static_cast<T*>(v_out);
-  a.q_weight = static_cast<const T*>(q_weight);
-  a.k_weight = static_cast<const T*>(k_weight);
+static int norm_typed(NormArgs<T> a, int32_t b, int count, float theta, hipStream_t stream) {
   NormFreq tab;
   for (int i = 0; i < 40; ++i) tab.w[i] = 0.0;
   if (a.rotate)
     for (int i = 0; i < D / 2; ++i) tab.w[i] = std::pow((double)theta, -2.0 * i / D);
-  return launch_norm<T, D, 1>(a, b, tab, stream);
+  // waves of one tensor with a head a thread
+  constexpr int RPW = 64 / (D / 2 / Piece<T>::E);
+  const int64_t waves = ((int64_t)b * a.H * a.n + RPW - 1) / RPW;
+  if (waves < NORM_SMALL) return launch_norm<T, D, 1, 1>(a, b, count, tab, stream);
+  if (count < 3 || waves < NORM_LARGE) return launch_norm<T, D, 4, 1>(a, b, count, tab, stream);
+  return launch_norm<T, D, sizeof(T) == 2 ? 4 : 2, 3>(a, b, count, tab, stream);
 }
 
 }  // namespace sckv
@@ -243,12 +286,29 @@ extern "C" int qk_norm_rope(const void* q, const void* k, const void* v, void* q
     return fail(SCKV_EINVAL, "qk_norm_rope: strides must be multiples of 16 bytes");
   if (n == 0) return SCKV_OK;
   auto go = [&](auto a) {
-    using T = std::remove_const_t<std::remove_pointer_t<decltype(a.q)>>;
+    using E = std::remove_pointer_t<decltype(+a.y[0])>;
+    const void* xs[3] = {q, k, v};
+    void* ys[3] = {q_out, k_out, v_out};
+    const void* ws[3] = {q_weight, k_weight, nullptr};
+    int count = 0;
+    for (int i = 0; i < 3; ++i) {
+      a.x[i] = nullptr;
+      a.y[i] = nullptr;
+      a.weight[i] = nullptr;
+      a.y_stride[i] = 0;
+      a.kind[i] = -1;
+    }
+    for (int i = 0; i < 3; ++i) {
+      if (!xs[i]) continue;
+      a.x[count] = static_cast<const E*>(xs[i]);
+      a.y[count] = static_cast<E*>(ys[i]);
+      a.weight[count] = static_cast<const E*>(ws[i]);
+      a.y_stride[count] = i == 0 ? q_out_stride_bh : kv_stride_bh;
+      a.kind[count++] = i;
+    }
     a.xb = x_stride_b;
     a.xh = x_stride_h;
     a.xr = x_stride_row;
-    a.q_out_s = q_out_stride_bh;
-    a.kv_s = kv_stride_bh;
     a.pos = pos;
     a.cur_tok = cur_tok;
     a.row0 = row0;
@@ -256,12 +316,12 @@ extern "C" int qk_norm_rope(const void* q, const void* k, const void* v, void* q
     a.eps = eps;
     a.H = H;
     a.n = n;
-    a.kv_rows = (k || v) ? kv_rows : n;
+    a.kv_rows = kv_rows;
     a.L_meta = L_meta;
     a.tok0 = tok0;
     a.rotate = theta > 0.f ? 1 : 0;
-    return d_head == 64 ? norm_typed<T, 64>(a, q, k, v, q_out, k_out, v_out, q_weight, k_weight, b, theta, stream)
-                        : norm_typed<T, 80>(a, q, k, v, q_out, k_out, v_out, q_weight, k_weight, b, theta, stream);
+    return d_head == 64 ? norm_typed<E, 64>(a, b, count, theta, stream)
+                        : norm_typed<E, 80>(a, b, count, theta, stream);
   };
   return dt == SCKV_BF16 ? go(NormArgs<uint16_t>()) : go(NormArgs<float>());
 }

@@ -71,79 +71,95 @@ static WeightPlan plan_at(void* ws, int32_t b, int32_t L_cap) {
 }
 
 constexpr int PLAN_WAVES = 16;
+constexpr int PLAN_U = 4;  // rows of a thread in flight
 constexpr int PLAN_THREADS = 64 * PLAN_WAVES;
 
 __global__ __launch_bounds__(PLAN_THREADS) void weight_plan_kernel(
     WeightPlan p, const int32_t* __restrict__ vu, int32_t L_meta, int32_t tok0, int32_t nq,
     const int32_t* __restrict__ kv_len, const int32_t* __restrict__ tok_idx, int32_t L_cap) {
-  __shared__ int counts[3][PLAN_WAVES];
+  constexpr int CHUNK = PLAN_THREADS * PLAN_U;
+  static_assert(PLAN_U * PLAN_WAVES == 64, "one wave scans the counts of a class");
+  // rows of class k that pass u of wave w holds, then those before them, at
+  // [k][u * PLAN_WAVES + w]; the chunk's total behind them
+  __shared__ int before[3][65];
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = min(max(kv_len[s], 0), L_cap);
   const int32_t* toks = tok_idx + (int64_t)s * L_cap;
   const int32_t* vus = vu + (int64_t)s * L_meta;
   const int64_t at = (int64_t)s * p.entries;
   const int last = tok0 + nq - 1;  // last query's token
-  // class of row r: 0 seen by every later query, 1 by some, 2 by none
-  auto classify = [&](int r, int& j, int& v, int& row) {
-    j = toks[r];
-    const bool known = j >= 0 && j < L_meta;
-    v = known ? vus[j] : -1;
-    row = r;
-    if (!known || v == j || j > last || v < tok0 || nq == 0) {
-      if (known && v == j && j >= tok0 && j <= last) row |= W_CL;
-      v = -1;
-      return 2;
+  // classes: 0 seen by every later query, 1 by some, 2 by none (3: no row)
+  int j[PLAN_U], v[PLAN_U], c[PLAN_U];
+  uint64_t m[3][PLAN_U];
+  auto classify = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < PLAN_U; ++u) j[u] = toks[min(base + u * PLAN_THREADS + tid, n - 1)];
+#pragma unroll
+    for (int u = 0; u < PLAN_U; ++u) v[u] = vus[min(max(j[u], 0), L_meta - 1)];
+#pragma unroll
+    for (int u = 0; u < PLAN_U; ++u) {
+      const bool none = j[u] < 0 || j[u] >= L_meta || v[u] == j[u] || j[u] > last || v[u] < tok0 || nq == 0;
+      c[u] = base + u * PLAN_THREADS + tid >= n ? 3 : none ? 2 : v[u] >= last ? 0 : 1;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) m[k][u] = __ballot(c[u] == k);
     }
-    return v >= last ? 0 : 1;
   };
-  // rows of each class, by wave; a wave's chunks are counted in registers
-  int mine[3] = {0, 0, 0};
-  for (int base = 0; base < n; base += PLAN_THREADS) {
-    int j, v, row, c = -1;
-    if (base + tid < n) c = classify(base + tid, j, v, row);
+  // a chunk's counts become exclusive prefix sums
+  auto scan = [&]() {
+    __syncthreads();  // those of the chunk before have been read
 #pragma unroll
-    for (int k = 0; k < 3; ++k) mine[k] += __popcll(__ballot(c == k));
+    for (int u = 0; u < PLAN_U; ++u) {
+      const int x0 = __popcll(m[0][u]), x1 = __popcll(m[1][u]), x2 = __popcll(m[2][u]);
+      if (lane < 3) before[lane][u * PLAN_WAVES + wave] = lane == 0 ? x0 : lane == 1 ? x1 : x2;
+    }
+    __syncthreads();
+    if (wave < 3) {
+      const int x = before[wave][lane];
+      int sum = x;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(sum, off, 64);
+        if (lane >= off) sum += y;
+      }
+      before[wave][lane] = sum - x;
+      if (lane == 63) before[wave][64] = sum;
+    }
+    __syncthreads();
+  };
+  // rows of each class
+  int total[3] = {0, 0, 0};
+  for (int base = 0; base < n; base += CHUNK) {
+    classify(base);
+    scan();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) total[k] += before[k][64];
   }
-  if (lane < 3) counts[lane][wave] = lane == 0 ? mine[0] : lane == 1 ? mine[1] : mine[2];
-  __syncthreads();
-  int total[3] = {0, 0, 0}, first[3];
-  for (int w = 0; w < PLAN_WAVES; ++w)
-#pragma unroll
-    for (int k = 0; k < 3; ++k) total[k] += counts[k][w];
-  __syncthreads();
-  int start = 0;
+  int start = 0, first[3], done[3];
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    first[k] = start;
+    first[k] = done[k] = start;
     start += (total[k] + W_CLASS - 1) / W_CLASS * W_CLASS;
   }
   // the rows, in order within each class
-  int done[3] = {first[0], first[1], first[2]};
-  for (int base = 0; base < n; base += PLAN_THREADS) {
-    int j = 0, v = 0, row = 0, c = -1;
-    if (base + tid < n) c = classify(base + tid, j, v, row);
-    uint64_t m[3];
-#pragma unroll
-    for (int k = 0; k < 3; ++k) m[k] = __ballot(c == k);
-    if (lane < 3) counts[lane][wave] = __popcll(lane == 0 ? m[0] : lane == 1 ? m[1] : m[2]);
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      int before = 0, all = 0;
-      for (int w = 0; w < PLAN_WAVES; ++w) {
-        const int x = counts[k][w];
-        before += w < wave ? x : 0;
-        all += x;
-      }
-      if (c == k) {
-        const int64_t e = at + done[k] + before + mask_rank(m[k]);
-        p.row[e] = row;
-        p.tok[e] = j;
-        p.vu[e] = v;
-      }
-      done[k] += all;
+  for (int base = 0; base < n; base += CHUNK) {
+    if (n > CHUNK) {  // (else they are still held)
+      classify(base);
+      scan();
     }
-    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < PLAN_U; ++u)
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (c[u] == k) {
+          const int row = base + u * PLAN_THREADS + tid;
+          const bool cl = k == 2 && v[u] == j[u] && j[u] >= tok0 && j[u] <= last;
+          const int64_t e = at + done[k] + before[k][u * PLAN_WAVES + wave] + mask_rank(m[k][u]);
+          p.row[e] = cl ? row | W_CL : row;
+          p.tok[e] = j[u];
+          p.vu[e] = k == 2 ? -1 : v[u];
+        }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) done[k] += before[k][64];
   }
   // what fills a class's last tiles: row -1, seen by none
 #pragma unroll
