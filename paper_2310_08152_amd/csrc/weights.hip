@@ -32,8 +32,8 @@
 namespace sckv {
 
 constexpr float W_LOG2E = 1.4426950408889634f;
-constexpr float W_RESCALE = 8.f;  // lazy maximum, log2 units
 constexpr int W_TILE = 32;        // rows, or queries, of a tile
+constexpr int W_WAVES = 4;        // of a workgroup
 constexpr int W_CLASS = 64;       // classes of the list start at multiples of this
 constexpr int W_CL = 1 << 20;     // list entry: a <CL> row among the queries' tokens
 
@@ -244,7 +244,36 @@ __device__ __forceinline__ float other_half(float x, bool sum) {
   return sum ? a + b : fmaxf(a, b);
 }
 
-constexpr int W_WAVES = 4;
+// maximum and sum of a query (by lane) over one more tile of scores.  The
+// maximum is only looked for where the weights of the tile, taken against the
+// one so far, leave a lane's sum above 2^16 (or where a lane has none yet):
+// sums then stay in range, and the comparison of 16 scores is spared.
+__device__ __forceinline__ void add_tile(const f32x16& sc, float c, float& M, float& l) {
+  const float m0 = M == -INFINITY ? 0.f : M;
+  float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+  for (int v = 0; v < 16; v += 2) {
+    a0 += fast_exp2(fmaf(sc[v], c, -m0));
+    a1 += fast_exp2(fmaf(sc[v + 1], c, -m0));
+  }
+  if (__any(!(a0 + a1 <= 65536.f) || M == -INFINITY)) {
+    float mb = sc[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) mb = fmaxf(mb, sc[v]);
+    const float mn = fmaxf(M, other_half(mb, false) * c);
+    l = mn == -INFINITY ? 0.f : l * fast_exp2(M - mn);
+    M = mn;
+    const float m1 = M == -INFINITY ? 0.f : M;
+    a0 = a1 = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; v += 2) {
+      a0 += fast_exp2(fmaf(sc[v], c, -m1));
+      a1 += fast_exp2(fmaf(sc[v + 1], c, -m1));
+    }
+  }
+  l += a0 + a1;
+}
+
 
 // ---------------------------------------------------------------------------
 // stats: (maximum, sum) of each query over the rows of one of `splits` shares
@@ -252,7 +281,7 @@ constexpr int W_WAVES = 4;
 // waves of a workgroup are units next to one another, which read the same keys.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int QT>
-__global__ __launch_bounds__(64 * W_WAVES) void weight_stats_kernel(
+__global__ __launch_bounds__(64 * W_WAVES, 2) void weight_stats_kernel(
     const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, float2* __restrict__ ml,
     int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c, const int32_t* __restrict__ vu,
     int32_t L_meta, int32_t tok0, int32_t n_slice, int32_t qtiles, int32_t splits) {
@@ -330,23 +359,7 @@ __global__ __launch_bounds__(64 * W_WAVES) void weight_stats_kernel(
       f32x16 sc = scores<T, D>(K, Q[x]);
       if (r.s.tmax > ta[x] || r.s.vmin < tb[x])
         mask_scores(sc, toks + r.t * W_TILE, vus + r.t * W_TILE, t[x], h);
-      float mb = sc[0];
-#pragma unroll
-      for (int v = 1; v < 16; ++v) mb = fmaxf(mb, sc[v]);
-      mb = other_half(mb, false) * c;
-      if (__any(mb > M[x] + W_RESCALE)) {
-        const float mn = fmaxf(M[x], mb);
-        l[x] = mn == -INFINITY ? 0.f : l[x] * fast_exp2(M[x] - mn);
-        M[x] = mn;
-      }
-      const float m0 = M[x] == -INFINITY ? 0.f : M[x];  // a lane that saw no row yet
-      float a0 = 0.f, a1 = 0.f;
-#pragma unroll
-      for (int v = 0; v < 16; v += 2) {
-        a0 += fast_exp2(fmaf(sc[v], c, -m0));
-        a1 += fast_exp2(fmaf(sc[v + 1], c, -m0));
-      }
-      l[x] += a0 + a1;
+      add_tile(sc, c, M[x], l[x]);
     }
   };
 
@@ -382,13 +395,40 @@ __global__ __launch_bounds__(64 * W_WAVES) void weight_stats_kernel(
   }
 }
 
+// the normaliser of query i, from the shares' maxima and sums (+inf: the query
+// gives nothing); the halves of the wave take every other share
+__device__ __forceinline__ float tile_lse(const float2* __restrict__ ml, int i, int nq, int splits,
+                                          int h) {
+  float m = -INFINITY, l = 0.f;
+  if (i < nq) {
+    if (splits == 1) {
+      const float2 x = ml[i];
+      m = x.x;
+      l = x.y;
+    } else {
+      for (int j = h; j < splits; j += 2) {
+        const float2 x = ml[(int64_t)j * nq + i];
+        const float mn = fmaxf(m, x.x);
+        if (mn != -INFINITY) l = l * fast_exp2(m - mn) + x.y * fast_exp2(x.x - mn);
+        m = mn;
+      }
+    }
+  }
+  if (splits > 1) {
+    const float mn = other_half(m, false);
+    l = other_half(m == -INFINITY ? 0.f : l * fast_exp2(m - mn), true);
+    m = mn;
+  }
+  return l > 0.f ? m + __builtin_amdgcn_logf(l) : INFINITY;
+}
+
 // ---------------------------------------------------------------------------
 // sums: KT tiles of rows a wave.  WQ = 1: the workgroup's waves take key tiles
 // of their own; WQ = W_WAVES: they share theirs and take every WQ-th tile of
 // queries each (launches of few keys).
 // ---------------------------------------------------------------------------
 template <typename T, int D, int KT, int WQ>
-__global__ __launch_bounds__(64 * W_WAVES) void weight_sums_kernel(
+__global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_kernel(
     const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, const float2* __restrict__ ml,
     const float* w_in, float* w_out, int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c,
     int32_t tok0, int32_t L_cap, int32_t n_slice, int32_t splits) {
@@ -424,32 +464,8 @@ __global__ __launch_bounds__(64 * W_WAVES) void weight_sums_kernel(
   const int qa = z < 0 || a > z ? 1 : max(a - tok0, 0) / W_TILE;
   const int qz = z < 0 || a > z ? 0 : (z - tok0) / W_TILE;
   const float2* mls = ml + (int64_t)slice * splits * nq;
-  // a tile's queries, and the lane's normaliser (+inf: gives nothing)
   auto load_q = [&](Operand<T, D>& Q, int qt) { Q.load(qb + (int64_t)min(qt * W_TILE + l32, nq - 1) * D, h); };
-  auto load_lse = [&](int qt) {
-    const int i = qt * W_TILE + l32;
-    float m = -INFINITY, l = 0.f;
-    if (i < nq) {
-      if (splits == 1) {
-        const float2 x = mls[i];
-        m = x.x;
-        l = x.y;
-      } else {  // the halves take every other share
-        for (int j = h; j < splits; j += 2) {
-          const float2 x = mls[(int64_t)j * nq + i];
-          const float mn = fmaxf(m, x.x);
-          if (mn != -INFINITY) l = l * fast_exp2(m - mn) + x.y * fast_exp2(x.x - mn);
-          m = mn;
-        }
-      }
-    }
-    if (splits > 1) {
-      const float mn = other_half(m, false);
-      l = other_half(m == -INFINITY ? 0.f : l * fast_exp2(m - mn), true);
-      m = mn;
-    }
-    return l > 0.f ? m + __builtin_amdgcn_logf(l) : INFINITY;
-  };
+  auto load_lse = [&](int qt) { return tile_lse(mls, qt * W_TILE + l32, nq, splits, h); };
   auto compute = [&](const Operand<T, D>& Q, float lse, int qt) {
     const int ta = tok0 + qt * W_TILE, tb = min(ta + W_TILE - 1, last);
 #pragma unroll
@@ -517,18 +533,419 @@ __global__ __launch_bounds__(64 * W_WAVES) void weight_sums_kernel(
   }
 }
 
-// Units of the stats launch: two waves a SIMD at least, where the queries (one
-// tile a wave then, else two) and up to 64 shares of the rows, of 128 at
-// least, give as many.
-constexpr int W_FILL = 2048;
-static int stats_tiles(bool bf16, int64_t slices, int32_t nq) {
-  return bf16 && slices * ((nq + 2 * W_TILE - 1) / (2 * W_TILE)) >= W_FILL / 2 ? 2 : 1;
+// ---------------------------------------------------------------------------
+// Stages: 64 rows (two tiles) that a workgroup's waves share through LDS,
+// for long lists: a wave's own loads of an operand touch 32 cache lines an
+// instruction, 32 bytes of each; staged, a line is read once a workgroup
+// (16384 queries, 32 heads of 64: 1180 -> 923 us).  Short lists are slower so
+// (16 x 1024 queries of 80: 152 -> 207 us): a workgroup's four waves go through
+// the union of their lists, a barrier a stage.
+// Piece g of row r lies at g ^ (r % 8) where a row is a power of two of
+// pieces, at g otherwise (rows of 160 and 320 bytes fall on different banks by
+// themselves), so that the 8 rows of a quarter wave's read share no bank.
+// ---------------------------------------------------------------------------
+template <typename T, int D>
+struct Stage {
+  static constexpr int ROWS = 2 * W_TILE;
+  static constexpr int PIECES = D * (int)sizeof(T) / 16;  // of a row
+  static constexpr int BYTES = ROWS * PIECES * 16;
+  static constexpr int THREADS = 64 * W_WAVES;
+  static constexpr int PER = (ROWS * PIECES + THREADS - 1) / THREADS;  // of a thread
+  __device__ __forceinline__ static int slot(int row, int g) {
+    return (PIECES & (PIECES - 1)) == 0 ? g ^ (row & 7) : g;
+  }
+  u32x4 x[PER];
+  // rows[i]: the row of the source that this thread's piece i belongs to
+  __device__ __forceinline__ void load(const T* src, const int* rows, int tid) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int g = (tid + i * THREADS) % PIECES;
+      x[i] = ld16(src + (int64_t)rows[i] * D + g * (16 / (int)sizeof(T)));
+    }
+  }
+  __device__ __forceinline__ static int row_of(int tid, int i) {  // of the stage (clamped)
+    return min((tid + i * THREADS) / PIECES, ROWS - 1);
+  }
+  __device__ __forceinline__ void store(char* lds, int tid) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = tid + i * THREADS, row = e / PIECES, g = e % PIECES;
+      if (e < ROWS * PIECES) st16(lds + (row * PIECES + slot(row, g)) * 16, x[i]);
+    }
+  }
+  // a tile's operand (rows 32 half .. of the stage)
+  __device__ __forceinline__ static void read(Operand<T, D>& o, const char* lds, int half, int lane) {
+    const int row = half * W_TILE + (lane & 31), h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < Operand<T, D>::N; ++i) o.x[i] = ld16(lds + (row * PIECES + slot(row, 2 * i + h)) * 16);
+  }
+};
+
+// stats of large launches: QT tiles of queries a wave, W_WAVES * QT a workgroup
+template <typename T, int D, int QT>
+__global__ __launch_bounds__(64 * W_WAVES, 2) void weight_stats_staged_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, float2* __restrict__ ml,
+    int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c, const int32_t* __restrict__ vu,
+    int32_t L_meta, int32_t tok0, int32_t n_slice, int32_t qgroups, int32_t splits) {
+  using S = Stage<T, D>;
+  __shared__ __align__(16) char lds[2][S::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wg = blockIdx.x / n_slice, slice = blockIdx.x - wg * n_slice;
+  const int split = wg % splits;
+  const int g0 = (qgroups - 1 - wg / splits) * W_WAVES * QT * W_TILE;  // first query; the last see most
+  const int s = slice / H;
+  const T* qb = q + slice * q_s;
+  const T* kb = k + slice * k_s;
+  const int64_t at = (int64_t)s * p.entries;
+  const TileSum* sums = p.sum + (int64_t)s * (p.entries / W_TILE);
+  const int n_stage = p.tiles[s].x / 2;
+  const int q0 = g0 + wave * QT * W_TILE;
+
+  Operand<T, D> Q[QT];
+  int t[QT], ta[QT], tb[QT];
+  float M[QT], l[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int i = q0 + W_TILE * x;
+    t[x] = tok0 + min(i + l32, nq - 1);
+    ta[x] = tok0 + i;
+    tb[x] = i < nq ? min(ta[x] + W_TILE - 1, tok0 + nq - 1) : -1;  // -1: sees nothing below
+    Q[x].load(qb + (int64_t)min(i + l32, nq - 1) * D, h);
+    M[x] = -INFINITY;
+    l[x] = 0.f;
+  }
+  // the share's stages that some query of the workgroup sees, 64 at a time
+  const int lo = tok0 + g0, hi = tok0 + min(g0 + W_WAVES * QT * W_TILE, nq) - 1;
+  TileSum held[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  int cand = 0, held0 = 0;
+  uint64_t seen = 0;
+  struct Ref {
+    int stage;
+    TileSum s[2];
+  };
+  auto next = [&]() {
+    while (seen == 0 && cand * splits + split < n_stage) {
+      const int st = (cand + lane) * splits + split;
+      held0 = cand;
+      cand += 64;
+      bool see = false;
+      if (st < n_stage) {
+        held[0] = sums[2 * st];
+        held[1] = sums[2 * st + 1];
+        see = (held[0].tmin <= hi && held[0].vmax >= lo) || (held[1].tmin <= hi && held[1].vmax >= lo);
+      }
+      seen = __ballot(see);
+    }
+    Ref r;
+    r.stage = -1;
+    if (seen != 0) {
+      const int i = __builtin_ctzll(seen);
+      seen &= seen - 1;
+      r.stage = (held0 + i) * splits + split;
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        r.s[y].tmin = __builtin_amdgcn_readlane(held[y].tmin, i);
+        r.s[y].tmax = __builtin_amdgcn_readlane(held[y].tmax, i);
+        r.s[y].vmin = __builtin_amdgcn_readlane(held[y].vmin, i);
+        r.s[y].vmax = __builtin_amdgcn_readlane(held[y].vmax, i);
+      }
+    }
+    return r;
+  };
+  S st;
+  int rows[S::PER];
+  auto number = [&](const Ref& r) {
+#pragma unroll
+    for (int i = 0; i < S::PER; ++i)
+      rows[i] = r.stage >= 0 ? max(p.row[at + (int64_t)r.stage * S::ROWS + S::row_of(tid, i)], 0) : 0;
+  };
+  Ref cur = next();
+  number(cur);
+  if (cur.stage >= 0) st.load(kb, rows, tid);
+  Ref nxt = next();
+  number(nxt);
+  int buf = 0;
+  while (cur.stage >= 0) {
+    st.store(lds[buf], tid);
+    if (nxt.stage >= 0) st.load(kb, rows, tid);
+    const Ref after = next();
+    number(after);
+    // one barrier a stage: the other buffer was read before the last one
+    __syncthreads();
+    Operand<T, D> K;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      S::read(K, lds[buf], y, lane);
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        if (cur.s[y].tmin > tb[x] || cur.s[y].vmax < ta[x]) continue;
+        f32x16 sc = scores<T, D>(K, Q[x]);
+        if (cur.s[y].tmax > ta[x] || cur.s[y].vmin < tb[x]) {
+          const int64_t e = at + (int64_t)cur.stage * S::ROWS + y * W_TILE;
+          mask_scores(sc, p.tok + e, p.vu + e, t[x], h);
+        }
+        add_tile(sc, c, M[x], l[x]);
+      }
+    }
+    cur = nxt;
+    nxt = after;
+    buf ^= 1;
+  }
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const float sum = other_half(l[x], true);
+    const int i = q0 + W_TILE * x + l32;
+    if (lane < 32 && i < nq) {
+      const bool cl = vu[(int64_t)s * L_meta + t[x]] == t[x];
+      ml[((int64_t)slice * splits + split) * nq + i] = cl ? make_float2(-INFINITY, 0.f) : make_float2(M[x], sum);
+    }
+  }
 }
-static int stats_splits(bool bf16, int64_t slices, int32_t nq, int32_t L_cap) {
-  const int qt = stats_tiles(bf16, slices, nq) * W_TILE;
-  const int64_t units = slices * ((nq + qt - 1) / qt);
-  const int64_t want = (W_FILL + units - 1) / std::max<int64_t>(units, 1);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, 64, (L_cap + 127) / 128}));
+
+// sums of large launches: KT tiles of rows a wave, W_WAVES * KT a workgroup
+template <typename T, int D, int KT>
+__global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, const float2* __restrict__ ml,
+    const float* w_in, float* w_out, int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c,
+    int32_t tok0, int32_t L_cap, int32_t n_slice, int32_t splits) {
+  using S = Stage<T, D>;
+  __shared__ __align__(16) char lds[2][S::BYTES];
+  __shared__ float lse[2][S::ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wg = blockIdx.x / n_slice, slice = blockIdx.x - wg * n_slice;
+  const int s = slice / H;
+  const int n_tiles = p.tiles[s].y;
+  const int g0 = wg * W_WAVES * KT;  // first tile of the workgroup
+  if (g0 >= n_tiles) return;
+  const T* qb = q + slice * q_s;
+  const T* kb = k + slice * k_s;
+  const int64_t at = (int64_t)s * p.entries;
+  const TileSum* sums = p.sum + (int64_t)s * (p.entries / W_TILE);
+  const int last = tok0 + nq - 1;
+  // the workgroup's first and last token that sees one of its rows
+  int a = 0x7fffffff, z = -1;
+  for (int i = g0; i < min(g0 + W_WAVES * KT, n_tiles); ++i) {
+    const TileSum x = sums[i];
+    if (x.vmax >= 0) {
+      a = min(a, x.tmin);
+      z = max(z, x.vmax);
+    }
+  }
+  z = min(z, last);
+  const bool some = z >= 0 && a <= z;
+  const int sa = some ? max(a - tok0, 0) / S::ROWS : 1, sz = some ? (z - tok0) / S::ROWS : 0;
+
+  const int t0 = g0 + wave * KT;
+  TileSum ts[KT];
+  Operand<T, D> K[KT];
+  f32x16 acc[KT];
+#pragma unroll
+  for (int x = 0; x < KT; ++x) {
+    const bool in = t0 + x < n_tiles;
+    ts[x] = in ? sums[t0 + x] : TileSum{0x7fffffff, 0x7fffffff, -1, -1};
+    const int e = in ? p.row[at + (int64_t)(t0 + x) * W_TILE + l32] : -1;
+    K[x].load(kb + (int64_t)(max(e, 0) & (W_CL - 1)) * D, h);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[x][v] = 0.f;
+  }
+  const float2* mls = ml + (int64_t)slice * splits * nq;
+  S st;
+  int rows[S::PER];
+  auto load = [&](int stage) {
+#pragma unroll
+    for (int i = 0; i < S::PER; ++i) rows[i] = min(stage * S::ROWS + S::row_of(tid, i), nq - 1);
+    st.load(qb, rows, tid);
+  };
+  // one wave takes the normalisers, 32 queries at a time
+  float n0 = 0.f, n1 = 0.f;
+  auto normalisers = [&](int stage) {
+    if (wave == 0) {
+      n0 = tile_lse(mls, stage * S::ROWS + l32, nq, splits, h);
+      n1 = tile_lse(mls, stage * S::ROWS + W_TILE + l32, nq, splits, h);
+    }
+  };
+  if (sa <= sz) {
+    load(sa);
+    normalisers(sa);
+  }
+  int buf = 0;
+  for (int g = sa; g <= sz; ++g) {
+    st.store(lds[buf], tid);
+    if (wave == 0) lse[buf][lane] = h ? n1 : n0;
+    if (g < sz) {
+      load(g + 1);
+      normalisers(g + 1);
+    }
+    __syncthreads();
+    Operand<T, D> Q;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int ta = tok0 + g * S::ROWS + y * W_TILE, tb = min(ta + W_TILE - 1, last);
+      if (ta > last) continue;
+      S::read(Q, lds[buf], y, lane);
+      const float ls = lse[buf][y * W_TILE + l32];
+#pragma unroll
+      for (int x = 0; x < KT; ++x) {
+        if (ts[x].tmin > tb || ts[x].vmax < ta) continue;
+        f32x16 sc = scores<T, D>(K[x], Q);
+        if (ts[x].tmax > ta || ts[x].vmin < tb) {
+          const int64_t e = at + (int64_t)(t0 + x) * W_TILE;
+          mask_scores(sc, p.tok + e, p.vu + e, ta + l32, h);
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[x][v] += fast_exp2(fmaf(sc[v], c, -ls));
+      }
+    }
+    buf ^= 1;
+  }
+#pragma unroll
+  for (int x = 0; x < KT; ++x) {
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = acc[x][i];
+    int base = 0;
+    half_wave_reduce<16, 16>(v, lane, base);
+    const int m = 8 * (base / 4) + 4 * h + base % 4;
+    const int e = t0 + x < n_tiles && !(lane & 1) ? p.row[at + (int64_t)(t0 + x) * W_TILE + m] : -1;
+    if (e < 0) continue;
+    const int64_t r = (int64_t)slice * L_cap + (e & (W_CL - 1));
+    w_out[r] = (w_in ? w_in[r] : 0.f) + (e & W_CL ? 1.f : v[0]);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// sums of few queries (QT tiles): a wave keeps all queries and streams `run`
+// key tiles, the next tile's keys and sums in flight while one is computed.
+// With the keys kept instead, a wave's chain of loads (row numbers, keys, old
+// sums) was paid every 64 rows: 49 us against VOTES_US for 32 queries over
+// 512 slices of 2050 rows of 80.
+// ---------------------------------------------------------------------------
+template <typename T, int D, int QT>
+__global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, const float2* __restrict__ ml,
+    const float* w_in, float* w_out, int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c,
+    int32_t tok0, int32_t L_cap, int32_t n_slice, int32_t splits, int32_t run) {
+  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+  const int wg = blockIdx.x / n_slice, slice = blockIdx.x - wg * n_slice;
+  const int unit = __builtin_amdgcn_readfirstlane(wg * W_WAVES + (threadIdx.x >> 6));
+  const int s = slice / H;
+  const int n_tiles = p.tiles[s].y;
+  const int t0 = unit * run, t1 = min(t0 + run, n_tiles);
+  if (t0 >= t1) return;
+  const T* kb = k + slice * k_s;
+  const int64_t at = (int64_t)s * p.entries;
+  const TileSum* sums = p.sum + (int64_t)s * (p.entries / W_TILE);
+  const float2* mls = ml + (int64_t)slice * splits * nq;
+  const int last = tok0 + nq - 1;
+  // the row of a tile whose sum this lane ends with
+  int base = 0;
+  {
+    float v[16] = {0.f};
+    half_wave_reduce<16, 16>(v, lane, base);
+  }
+  const int m = 8 * (base / 4) + 4 * h + base % 4;
+
+  Operand<T, D> A, B;
+  auto number = [&](int t, int i) { return p.row[at + (int64_t)min(t, t1 - 1) * W_TILE + i]; };
+  auto load = [&](Operand<T, D>& K, int e) { K.load(kb + (int64_t)(max(e, 0) & (W_CL - 1)) * D, h); };
+  const int64_t wo = (int64_t)slice * L_cap;
+  auto old = [&](int e) { return w_in ? w_in[wo + (max(e, 0) & (W_CL - 1))] : 0.f; };
+  int e0 = number(t0, m), e1 = number(t0 + 1, m);
+  int i1 = number(t0 + 1, l32);
+  load(A, number(t0, l32));
+  float o0 = old(e0);
+  Operand<T, D> Q[QT];
+  float lse[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    Q[x].load(q + slice * q_s + (int64_t)min(W_TILE * x + l32, nq - 1) * D, h);
+    lse[x] = tile_lse(mls, W_TILE * x + l32, nq, splits, h);
+  }
+  auto compute = [&](const Operand<T, D>& K, int t, int e, float before) {
+    const TileSum ts = sums[t];
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+      const int ta = tok0 + W_TILE * x, tb = min(ta + W_TILE - 1, last);
+      if (ts.tmin > tb || ts.vmax < ta) continue;
+      f32x16 sc = scores<T, D>(K, Q[x]);
+      if (ts.tmax > ta || ts.vmin < tb)
+        mask_scores(sc, p.tok + at + t * W_TILE, p.vu + at + t * W_TILE, ta + l32, h);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] += fast_exp2(fmaf(sc[i], c, -lse[x]));
+    }
+    int unused = 0;
+    half_wave_reduce<16, 16>(v, lane, unused);
+    if (!(lane & 1) && e >= 0)
+      w_out[wo + (e & (W_CL - 1))] = before + (e & W_CL ? 1.f : v[0]);
+  };
+  for (int t = t0; t < t1; t += 2) {
+    load(B, i1);
+    const int i2 = number(t + 2, l32);
+    const float o1 = old(e1);
+    const int e2 = number(t + 2, m);
+    compute(A, t, e0, o0);
+    if (t + 1 >= t1) break;
+    load(A, i2);
+    i1 = number(t + 3, l32);
+    o0 = old(e2);
+    const int e3 = number(t + 3, m);
+    compute(B, t + 1, e1, o1);
+    e0 = e2;
+    e1 = e3;
+  }
+}
+
+// Launch shapes, by sizes alone (us; rows are the cache's capacity, the host's
+// only hint of its length):
+//  * stats: a wave keeps two tiles of bf16 queries where that leaves W_UNITS
+//    waves (16 x 64 queries over 2048 rows of 64: 72 with one tile, 65 with two;
+//    32 heads of 2048 tokens: 74, 67), else one.  The rows are cut into
+//    up to 64 shares of at least 128 until there are W_FILL waves, two a SIMD.
+//  * sums: up to 32 queries (bf16: 64) are kept by every wave, which streams
+//    rows (`votes`: as many waves as stay resident, up to 16 tiles each).
+//    Beyond, a wave keeps two tiles of bf16 rows where W_FILL waves do, else
+//    one, and the waves of a workgroup share theirs below W_SHARE tiles (32
+//    heads of 2048 tokens: 93 a wave each, 74 shared).
+//  * from W_LONG rows and W_LONG / 4 queries on, with W_WGS workgroups: both
+//    staged in LDS.
+constexpr int W_FILL = 2048;
+constexpr int W_UNITS = 512;
+constexpr int W_SHARE = 4096;
+constexpr int W_RESIDENT = 3072;
+constexpr int W_LONG = 4096;
+constexpr int W_WGS = 512;
+
+struct WeightShape {
+  bool staged;
+  int votes;   // tiles of queries that every wave of the second pass keeps (0: not so)
+  int keep;    // tiles of queries that a wave of the first pass keeps
+  int qtiles;  // units of queries (workgroups' where staged, else waves')
+  int splits;  // shares of the rows in the first pass
+};
+static WeightShape weight_shape(bool bf16, int64_t slices, int32_t nq, int32_t L_cap) {
+  WeightShape w = {false, 0, 1, 0, 1};
+  if (nq == 0) return w;
+  const int two = bf16 ? 2 : 1;
+  w.votes = nq <= W_TILE ? 1 : nq <= two * W_TILE ? 2 : 0;
+  const int group = W_WAVES * W_TILE * two;
+  const int64_t groups = (nq + group - 1) / group;
+  w.staged = nq >= W_LONG / 4 && L_cap >= W_LONG && slices * groups >= W_WGS;
+  if (w.staged) {
+    w.keep = two;
+    w.qtiles = (int)groups;
+    return w;
+  }
+  const int pair = two * W_TILE;
+  if (nq > W_TILE && slices * ((nq + pair - 1) / pair) >= W_UNITS) w.keep = two;
+  w.qtiles = (nq + w.keep * W_TILE - 1) / (w.keep * W_TILE);
+  const int64_t units = slices * w.qtiles, want = (W_FILL + units - 1) / units;
+  w.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, 64, (L_cap + 127) / 128}));
+  return w;
 }
 
 template <typename T, int D>
@@ -537,51 +954,68 @@ static int launch_weights(const void* q, const void* k, const float* w_in, float
                           const int32_t* vu, int32_t L_meta, int32_t tok0, const int32_t* kv_len,
                           const int32_t* tok_idx, int32_t L_cap, void* ws, hipStream_t stream) {
   constexpr bool BF16 = sizeof(T) == 2;
+  constexpr int NT = BF16 ? 2 : 1;
+  constexpr int THREADS = 64 * W_WAVES;
   const T* qq = static_cast<const T*>(q);
   const T* kk = static_cast<const T*>(k);
   const WeightPlan p = plan_at(ws, b, L_cap);
   float2* ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan_bytes(b, L_cap));
   const int slices = b * H;
   const float c = scale * W_LOG2E;
+  const WeightShape sh = weight_shape(BF16, slices, nq, L_cap);
   weight_plan_kernel<<<b, PLAN_THREADS, 0, stream>>>(p, vu, L_meta, tok0, nq, kv_len, tok_idx, L_cap);
   int rc = hip_check(hipGetLastError(), "cached_attn_weights: plan launch");
   if (rc) return rc;
-  const int splits = nq > 0 ? stats_splits(BF16, slices, nq, L_cap) : 1;
+  unsigned g = 0;  // workgroups
+  auto grid = [&](int64_t per_slice) {
+    const int64_t n = per_slice * slices;
+    g = (unsigned)n;
+    return n > 0x7fffffff ? fail(SCKV_EUNSUP, "cached_attn_weights: too many tiles") : SCKV_OK;
+  };
   if (nq > 0) {
-    const int qt = stats_tiles(BF16, slices, nq);
-    const int qtiles = (nq + qt * W_TILE - 1) / (qt * W_TILE);
-    const int64_t wgs = (int64_t)slices * (((int64_t)qtiles * splits + W_WAVES - 1) / W_WAVES);
-    if (wgs > 0x7fffffff) return fail(SCKV_EUNSUP, "cached_attn_weights: too many tiles");
+    const int64_t units = (int64_t)sh.qtiles * sh.splits;
+    rc = grid(sh.staged ? units : (units + W_WAVES - 1) / W_WAVES);
+    if (rc) return rc;
     auto go = [&](auto kernel) {
-      kernel<<<(unsigned)wgs, 64 * W_WAVES, 0, stream>>>(qq, kk, p, ml, H, nq, q_s, k_s, c, vu, L_meta,
-                                                         tok0, slices, qtiles, splits);
+      kernel<<<g, THREADS, 0, stream>>>(qq, kk, p, ml, H, nq, q_s, k_s, c, vu, L_meta, tok0, slices,
+                                        sh.qtiles, sh.splits);
     };
-    if constexpr (BF16) {
-      if (qt == 2) go(weight_stats_kernel<T, D, 2>);
-      else go(weight_stats_kernel<T, D, 1>);
-    } else {
-      go(weight_stats_kernel<T, D, 1>);
-    }
+    if (sh.staged) go(weight_stats_staged_kernel<T, D, NT>);
+    else if (sh.keep == NT) go(weight_stats_kernel<T, D, NT>);
+    else go(weight_stats_kernel<T, D, 1>);
     rc = hip_check(hipGetLastError(), "cached_attn_weights: stats launch");
     if (rc) return rc;
   }
-  // Two key tiles a wave read the queries half as often; one where that leaves
-  // SIMDs idle, shared by the workgroup's waves where it still does.
   const int64_t tiles = p.entries / W_TILE;
-  const int kt = BF16 && slices * (tiles / 2) >= W_FILL ? 2 : 1;
-  const int wq = kt == 1 && slices * tiles < W_FILL && nq > W_TILE ? W_WAVES : 1;
-  const int64_t per_wg = (int64_t)kt * (W_WAVES / wq);
-  const int64_t wgs = slices * ((tiles + per_wg - 1) / per_wg);
-  if (wgs > 0x7fffffff) return fail(SCKV_EUNSUP, "cached_attn_weights: too many tiles");
   auto go = [&](auto kernel) {
-    kernel<<<(unsigned)wgs, 64 * W_WAVES, 0, stream>>>(qq, kk, p, ml, w_in, w_out, H, nq, q_s, k_s, c,
-                                                       tok0, L_cap, slices, splits);
+    kernel<<<g, THREADS, 0, stream>>>(qq, kk, p, ml, w_in, w_out, H, nq, q_s, k_s, c, tok0, L_cap,
+                                      slices, sh.splits);
   };
-  if constexpr (BF16) {
-    if (kt == 2) go(weight_sums_kernel<T, D, 2, 1>);
+  if (sh.votes > 0) {
+    const int run = (int)std::min<int64_t>(16, std::max<int64_t>(1, slices * tiles / W_RESIDENT));
+    const int64_t units = (tiles + run - 1) / run;
+    rc = grid((units + W_WAVES - 1) / W_WAVES);
+    if (rc) return rc;
+    auto vote = [&](auto kernel) {
+      kernel<<<g, THREADS, 0, stream>>>(qq, kk, p, ml, w_in, w_out, H, nq, q_s, k_s, c, tok0, L_cap,
+                                        slices, sh.splits, run);
+    };
+    if (sh.votes == NT) vote(weight_votes_kernel<T, D, NT>);
+    else vote(weight_votes_kernel<T, D, 1>);
+  } else if (sh.staged) {
+    rc = grid((tiles + W_WAVES * NT - 1) / (W_WAVES * NT));
+    if (rc) return rc;
+    go(weight_sums_staged_kernel<T, D, NT>);
+  } else {
+    const int kt = slices * (tiles / NT) >= W_FILL ? NT : 1;
+    const int wq = kt == 1 && slices * tiles < W_SHARE ? W_WAVES : 1;
+    const int64_t per_wg = (int64_t)kt * (W_WAVES / wq);
+    rc = grid((tiles + per_wg - 1) / per_wg);
+    if (rc) return rc;
+    if (wq > 1) go(weight_sums_kernel<T, D, 1, W_WAVES>);
+    else if (kt == NT) go(weight_sums_kernel<T, D, NT, 1>);
+    else go(weight_sums_kernel<T, D, 1, 1>);
   }
-  if (kt == 1 && wq == 1) go(weight_sums_kernel<T, D, 1, 1>);
-  if (kt == 1 && wq > 1) go(weight_sums_kernel<T, D, 1, W_WAVES>);
   return hip_check(hipGetLastError(), "cached_attn_weights: sums launch");
 }
 
@@ -594,7 +1028,8 @@ extern "C" size_t sckv_attn_weights_workspace_bytes(int32_t b, int32_t H, int32_
   if (b <= 0 || H <= 0 || nq < 0 || L_cap <= 0) return 0;
   // (the size function is not told the element type)
   const int64_t slices = (int64_t)b * H;
-  const int splits = std::max(stats_splits(true, slices, nq, L_cap), stats_splits(false, slices, nq, L_cap));
+  const int splits = std::max(weight_shape(true, slices, nq, L_cap).splits,
+                              weight_shape(false, slices, nq, L_cap).splits);
   return plan_bytes(b, L_cap) + (size_t)slices * splits * nq * sizeof(float2);
 }
 

@@ -77,6 +77,8 @@ CASES = [
     (1, 1, 64, "bf16", 3000, 129, True, 0.1),
     (4, 64, 64, "bf16", 530, 530, False, 0.5),    # two tiles of queries and of rows a wave
     (4, 64, 80, "bf16", 300, 131, True, 0.4),
+    (1, 64, 64, "bf16", 4100, 2100, False, 0.6),  # staged
+    (1, 110, 80, "f32", 4100, 1030, True, 0.2),
     (40, 13, 64, "bf16", 520, 5, False, 0.3),     # two tiles of rows, one of queries
     (3, 100, 80, "f32", 260, 45, False, 0.5),
 ]
