@@ -68,6 +68,7 @@ constexpr int DEC_ONE_MAX_ROWS = 1536;
 constexpr int DEC_SINGLE_MIN = 512;
 constexpr int DEC_NARROW_MIN = 1024;
 constexpr int DEC_WAVES_PER_SIMD = 2;  // decode_mfma_kernel's occupancy (its register count)
+constexpr size_t SCORE_LDS = 144 << 10;  // of a CU's 160 KB, for the scores of its workgroups
 constexpr int DEC_SPEC2_ROWS = 512;    // cache rows per wave from which two blocks are speculated
 
 // compute units of the current device, asked once per device
@@ -138,16 +139,37 @@ struct StepOnly {
 };
 // Adds the step's softmax weights to each row's accumulated weight.  A row's
 // weight needs the whole slice's maximum and sum, so the scores (log2 units)
-// are kept in `scores` and turned into weights once those are known: by the
-// slice's own workgroup where there is one, else by workgroups of the merge.
-// 4 bytes written and 4 read a row (mostly from the L2) beside the 4 * d that
-// the row itself takes in bf16; computing the scores again would read the keys
-// twice.
+// are kept and turned into weights once those are known: by the slice's own
+// workgroup where there is one, else by workgroups of the merge.  They are
+// kept in LDS where one workgroup has the slice and the cache's capacity fits
+// (`in_lds`), else in `scores`; computing them again would read the keys twice.
 struct StepWeights {
   static constexpr bool WEIGHTS = true, PREFIX = false;
   const float* w_in;
   float* w_out;
   float* scores;  // [slice][L_cap]
+  int32_t in_lds;
+};
+extern __shared__ float lds_scores[];  // [L_cap] (StepWeights, in_lds)
+
+// keeps the score of a slice's row r
+__device__ __forceinline__ void keep_score(const StepWeights& x, int64_t at, int r, float score) {
+  if (x.in_lds) lds_scores[r] = score;
+  else x.scores[at + r] = score;
+}
+
+// The first OLD_SUMS of a thread's accumulated weights, asked for before the
+// workgroup's merge and used after it.
+constexpr int OLD_SUMS = 8;
+struct OldSums {
+  float v[OLD_SUMS];
+  __device__ __forceinline__ void load(const StepWeights& x, int64_t at, int n, int tid, int nthr) {
+#pragma unroll
+    for (int i = 0; i < OLD_SUMS; ++i) {
+      const int r = tid + i * nthr;
+      v[i] = x.w_in && r < n ? x.w_in[at + r] : 0.f;
+    }
+  }
 };
 // Joins the partials of a shared prefix (one per chunk of it) to the slice's.
 struct StepPrefix {
@@ -166,12 +188,27 @@ __device__ __forceinline__ void keep_weights(const StepWeights& x, int64_t at, i
 // w_out of rows [r0, r1) of a slice of n cache rows and the new one, from the
 // slice's maximum M (log2 units) and sum of weights L
 __device__ __forceinline__ void add_weights(const StepWeights& x, int64_t at, int n, int r0, int r1,
-                                            float M, float L, int tid, int nthr) {
+                                            float M, float L, int tid, int nthr,
+                                            const OldSums* first = nullptr) {
   const float inv = 1.f / L;
-#pragma unroll 4
-  for (int r = r0 + tid; r < r1; r += nthr) {
-    const float old = x.w_in && r < n ? x.w_in[at + r] : 0.f;
-    x.w_out[at + r] = fmaf(exp2f(x.scores[at + r] - M), inv, old);
+  for (int base = r0 + tid; base < r1; base += OLD_SUMS * nthr) {
+    OldSums old;
+    float sc[OLD_SUMS];
+    if (first && base == r0 + tid) {
+      old = *first;
+    } else {
+      old.load(x, at, n, base, nthr);
+    }
+#pragma unroll
+    for (int i = 0; i < OLD_SUMS; ++i) {
+      const int r = min(base + i * nthr, r1 - 1);
+      sc[i] = x.in_lds ? lds_scores[r] : x.scores[at + r];
+    }
+#pragma unroll
+    for (int i = 0; i < OLD_SUMS; ++i) {
+      const int r = base + i * nthr;
+      if (r < r1) x.w_out[at + r] = fmaf(fast_exp2(sc[i] - M), inv, old.v[i]);
+    }
   }
 }
 
@@ -345,7 +382,7 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
       const int row = base + u * RPW + g;
       sc[u] = row < rc ? d : -INFINITY;
       if constexpr (X::WEIGHTS)
-        if (row < rc && seg == 0) x.scores[(int64_t)bh * L_cap + row] = d;
+        if (row < rc && seg == 0) keep_score(x, (int64_t)bh * L_cap, row, d);
     }
     float mx = m;
 #pragma unroll
@@ -385,7 +422,7 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
     for (int e = 0; e < E; ++e) d = fmaf(qf[e], kf[e], d);
     d = group_sum<GRP>(d);
     if constexpr (X::WEIGHTS)
-      if (seg == 0) x.scores[(int64_t)bh * L_cap + n] = d;
+      if (seg == 0) keep_score(x, (int64_t)bh * L_cap, n, d);
     const float mx = fmaxf(m, d);
     const float alpha = exp2f(m - mx);
     const float p = exp2f(d - mx);
@@ -400,6 +437,8 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
     }
   }
 
+  OldSums old;
+  if constexpr (FINAL && X::WEIGHTS) old.load(x, (int64_t)bh * L_cap, n, tid, THREADS);
   // merge the lane groups of the workgroup into this chunk's partial
   __shared__ float sm[NG], sl[NG];
   __shared__ float sacc[NG][D];
@@ -424,7 +463,7 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
     }
     if constexpr (FINAL && X::PREFIX) join_prefix<D>(x, bh, tid, M, Lsum, ov);
     if constexpr (FINAL && X::WEIGHTS)
-      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, M, Lsum, tid, THREADS);
+      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, M, Lsum, tid, THREADS, &old);
     if (tid >= D) {
     } else if constexpr (FINAL) {
       res[tid] = ov / Lsum;
@@ -779,7 +818,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     const int row = r0 + 32 * i + kr;
     const float sc = (row < rc && row != slot) ? c[0] * qscale : -INFINITY;
     if constexpr (X::WEIGHTS)
-      if (h == 0 && row < rc) x.scores[(int64_t)bh * L_cap + row] = sc;
+      if (h == 0 && row < rc) keep_score(x, (int64_t)bh * L_cap, row, sc);
     const float p = weigh(sc);
     if (h == 0) l += p;
 #pragma unroll
@@ -803,7 +842,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     const float p = weigh(sc);
     if (lane == 0) l += p;
     if constexpr (X::WEIGHTS)
-      if (lane == 0) x.scores[(int64_t)bh * L_cap + n] = sc;
+      if (lane == 0) keep_score(x, (int64_t)bh * L_cap, n, sc);
     if (kr == 0) {
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
@@ -832,6 +871,8 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
   if (i + NW < nblk) compute(i + NW, kB, vB);
   if (i + 2 * NW < nblk) compute(i + 2 * NW, kA, vA);
 
+  OldSums old;
+  if constexpr (FINAL && X::WEIGHTS) old.load(x, (int64_t)bh * L_cap, n, tid, THREADS);
   // wave partials: l over the wave, values over each half-wave
   l = wave_sum(l);
   int base = 0;
@@ -861,7 +902,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     }
     if constexpr (FINAL && X::PREFIX) join_prefix<D>(x, bh, tid, Mx, Ls, ov);
     if constexpr (FINAL && X::WEIGHTS)
-      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, Mx, Ls, tid, THREADS);
+      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, Mx, Ls, tid, THREADS, &old);
     if (tid >= D) {
     } else if constexpr (FINAL) {
       o[(int64_t)bh * D + tid] = f32_to_bf16(ov / Ls);
@@ -904,6 +945,15 @@ static int launch_decode(const void* q, const void* k_new, const void* v_new, vo
   const float qs = scale * LOG2E;
   const int slices = b * H;
   const FastDiv by_H = make_div((uint32_t)H), by_slices = make_div((uint32_t)slices);
+  size_t lds = 0;
+  // scores in LDS where all workgroups that a CU holds (`waves` of `of`) fit
+  auto room = [&](int waves, int of) {
+    if constexpr (X::WEIGHTS) {
+      const size_t need = (size_t)L_cap * sizeof(float);
+      x.in_lds = need <= (64 << 10) && need * (of / waves) <= SCORE_LDS;
+      lds = x.in_lds ? need : 0;
+    }
+  };
   if (one_workgroup(sizeof(T) == 2, slices, L_cap)) {
     const bool narrow = slices >= DEC_NARROW_MIN;
     if constexpr (sizeof(T) == 2) {
@@ -920,8 +970,9 @@ static int launch_decode(const void* q, const void* k_new, const void* v_new, vo
       // before the slice length arrives (rows past a shorter slice are read
       // for nothing, never used).
       const bool spec2 = ring == 0 && (int64_t)L_cap >= (int64_t)DEC_SPEC2_ROWS * nw;
+      room(nw, 4 * DEC_WAVES_PER_SIMD);
 #define SCKV_DECODE_LAUNCH(DD, NWW, SP)                                                          \
-  decode_mfma_kernel<DD, NWW, true, SP, X><<<slices, NWW * 64, 0, stream>>>(                      \
+  decode_mfma_kernel<DD, NWW, true, SP, X><<<slices, NWW * 64, lds, stream>>>(                    \
       qq, kn, vn, kc, vc, kv_len, cur_tok, vu, pos, L_meta, H, L_cap, qs, rotate, tab, part, 1,  \
       by_H, by_slices, slices, Split{1, 1}, out, status, ring, x)
       constexpr int D1 = D <= 64 ? D : 64;  // nw == 1 only where D <= 64
@@ -933,12 +984,13 @@ static int launch_decode(const void* q, const void* k_new, const void* v_new, vo
       else SCKV_DECODE_LAUNCH(D, 4, false);
 #undef SCKV_DECODE_LAUNCH
     } else {
+      room(narrow ? 4 : 8, 24);
       if (narrow)
-        decode_chunk_kernel<T, D, 256, true, X><<<slices, 256, 0, stream>>>(
+        decode_chunk_kernel<T, D, 256, true, X><<<slices, 256, lds, stream>>>(
             qq, kn, vn, kc, vc, kv_len, cur_tok, vu, pos, L_meta, H, L_cap, qs, rotate, tab, part,
             1, slices, Split{1, 1}, out, status, x);
       else
-        decode_chunk_kernel<T, D, 512, true, X><<<slices, 512, 0, stream>>>(
+        decode_chunk_kernel<T, D, 512, true, X><<<slices, 512, lds, stream>>>(
             qq, kn, vn, kc, vc, kv_len, cur_tok, vu, pos, L_meta, H, L_cap, qs, rotate, tab, part,
             1, slices, Split{1, 1}, out, status, x);
     }
@@ -1168,7 +1220,7 @@ extern "C" int compacted_decode_attn_weights(
   if (ws_bytes < sckv_decode_weights_workspace_bytes(b, H, L_cap, d_head))
     return fail(SCKV_EINVAL, W + ": workspace too small");
   const size_t part = partial_bytes(b, H, L_cap, d_head);
-  const StepWeights x = {w_in, w_out, reinterpret_cast<float*>(static_cast<char*>(ws) + part)};
+  const StepWeights x = {w_in, w_out, reinterpret_cast<float*>(static_cast<char*>(ws) + part), 0};
   return decode_dispatch(q, k_new, v_new, k_cache, v_cache, kv_len, cur_tok, vu, pos, L_meta, o, b,
                          H, L_cap, d_head, dt, scale, rope_theta, ws, part, status, stream, x);
 }
