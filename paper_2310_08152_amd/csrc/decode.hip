@@ -212,27 +212,43 @@ __device__ __forceinline__ void add_weights(const StepWeights& x, int64_t at, in
   }
 }
 
-// element e's share of the prefix partials joined to a slice's maximum M, sum
-// L and unnormalised output ov
+// Element e's share of a slice's prefix partials: the first ones are asked for
+// ahead of the workgroup's merge.
 template <int D>
-__device__ __forceinline__ void join_prefix(const StepPrefix& x, int bh, int e, float& M, float& L,
-                                            float& ov) {
-  const float* o = x.o + (int64_t)bh * x.n * D;
-  const float2* ml = x.ml + (int64_t)bh * x.n;
-  float Mx = M;
-#pragma unroll 4
-  for (int c = 0; c < x.n; ++c) Mx = fmaxf(Mx, ml[c].x);
-  const float f = exp2f(M - Mx);  // M is finite: the slice holds the new row
-  L *= f;
-  ov *= f;
-#pragma unroll 4
-  for (int c = 0; c < x.n; ++c) {
-    const float w = exp2f(ml[c].x - Mx);  // 0 for a chunk without rows (its maximum -inf)
-    L = fmaf(ml[c].y, w, L);
-    ov = fmaf(o[c * D + e], w, ov);
+struct PrefixParts {
+  static constexpr int FIRST = 4;
+  float2 ml[FIRST];
+  float o[FIRST];
+  __device__ __forceinline__ void load(const StepPrefix& x, int bh, int e, int c0) {
+#pragma unroll
+    for (int i = 0; i < FIRST; ++i) {
+      const int64_t c = (int64_t)bh * x.n + min(c0 + i, x.n - 1);
+      ml[i] = x.ml[c];
+      o[i] = x.o[c * D + e];
+    }
   }
-  M = Mx;
-}
+  // joins them to the slice's maximum M, sum L and unnormalised output ov
+  __device__ __forceinline__ void join(const StepPrefix& x, int bh, int e, float& M, float& L,
+                                       float& ov) {
+    for (int c0 = 0; c0 < x.n; c0 += FIRST) {
+      if (c0 > 0) load(x, bh, e, c0);
+      float Mx = M;
+#pragma unroll
+      for (int i = 0; i < FIRST; ++i) Mx = fmaxf(Mx, ml[i].x);
+      const float f = exp2f(M - Mx);  // M is finite: the slice holds the new row
+      L *= f;
+      ov *= f;
+#pragma unroll
+      for (int i = 0; i < FIRST; ++i) {
+        // 0 for a chunk without rows (its maximum -inf) and past the last one
+        const float w = c0 + i < x.n ? exp2f(ml[i].x - Mx) : 0.f;
+        L = fmaf(ml[i].y, w, L);
+        ov = fmaf(o[i], w, ov);
+      }
+      M = Mx;
+    }
+  }
+};
 
 // 0: ordinary append step; 1: <CL> step; 2: token outside [0, L_meta);
 // 3: no room for the new row
@@ -439,6 +455,8 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
 
   OldSums old;
   if constexpr (FINAL && X::WEIGHTS) old.load(x, (int64_t)bh * L_cap, n, tid, THREADS);
+  PrefixParts<D> pre;
+  if constexpr (FINAL && X::PREFIX) pre.load(x, bh, min(tid, D - 1), 0);
   // merge the lane groups of the workgroup into this chunk's partial
   __shared__ float sm[NG], sl[NG];
   __shared__ float sacc[NG][D];
@@ -461,7 +479,7 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
       Lsum += sl[i] * w;
       ov += sacc[i][e] * w;
     }
-    if constexpr (FINAL && X::PREFIX) join_prefix<D>(x, bh, tid, M, Lsum, ov);
+    if constexpr (FINAL && X::PREFIX) pre.join(x, bh, tid, M, Lsum, ov);
     if constexpr (FINAL && X::WEIGHTS)
       add_weights(x, (int64_t)bh * L_cap, n, 0, rows, M, Lsum, tid, THREADS, &old);
     if (tid >= D) {
@@ -543,6 +561,8 @@ __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
       return;
     }
   }
+  PrefixParts<D> pre;
+  if constexpr (X::PREFIX) pre.load(x, bh, min(tid, D - 1), 0);
   constexpr int PER = (D + 63) / 64;  // output elements per lane
   float M = -INFINITY, lsum = 0.f, acc[PER];
 #pragma unroll
@@ -582,7 +602,7 @@ __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < COMBINE_WAVES; ++w) v += sums[w][tid];
-    if constexpr (X::PREFIX) join_prefix<D>(x, bh, tid, M, lsum, v);
+    if constexpr (X::PREFIX) pre.join(x, bh, tid, M, lsum, v);
     v /= lsum;
     if constexpr (sizeof(T) == 2) o[(int64_t)bh * D + tid] = f32_to_bf16(v);
     else o[(int64_t)bh * D + tid] = v;
@@ -873,6 +893,8 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
 
   OldSums old;
   if constexpr (FINAL && X::WEIGHTS) old.load(x, (int64_t)bh * L_cap, n, tid, THREADS);
+  PrefixParts<D> pre;
+  if constexpr (FINAL && X::PREFIX) pre.load(x, bh, min(tid, D - 1), 0);
   // wave partials: l over the wave, values over each half-wave
   l = wave_sum(l);
   int base = 0;
@@ -900,7 +922,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
       Ls += any ? sl[w] * f : 0.f;
       ov += any ? sacc[w][e] * f : 0.f;
     }
-    if constexpr (FINAL && X::PREFIX) join_prefix<D>(x, bh, tid, Mx, Ls, ov);
+    if constexpr (FINAL && X::PREFIX) pre.join(x, bh, tid, Mx, Ls, ov);
     if constexpr (FINAL && X::WEIGHTS)
       add_weights(x, (int64_t)bh * L_cap, n, 0, rows, Mx, Ls, tid, THREADS, &old);
     if (tid >= D) {
@@ -1230,9 +1252,9 @@ extern "C" int compacted_decode_attn_weights(
 // the prefixes' partials
 // ---------------------------------------------------------------------------
 // (the size function is not told the element type)
-static int most_chunks(int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap) {
-  return std::max(prefix_chunks(true, n_prefix, H, per, P_cap),
-                  prefix_chunks(false, n_prefix, H, per, P_cap));
+static int most_chunks(int32_t d, int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap) {
+  return std::max(prefix_chunks(true, d, n_prefix, H, per, P_cap),
+                  prefix_chunks(false, d, n_prefix, H, per, P_cap));
 }
 
 extern "C" size_t sckv_shared_decode_workspace_bytes(int32_t b, int32_t H, int32_t n_prefix,
@@ -1241,7 +1263,7 @@ extern "C" size_t sckv_shared_decode_workspace_bytes(int32_t b, int32_t H, int32
   if (b <= 0 || H <= 0 || n_prefix <= 0 || P_cap <= 0 || L_cap <= 0 || d_head <= 0 || b % n_prefix)
     return 0;
   return partial_bytes(b, H, L_cap, d_head) +
-         (size_t)b * H * most_chunks(n_prefix, H, b / n_prefix, P_cap) * (d_head + 2) * sizeof(float);
+         (size_t)b * H * most_chunks(d_head, n_prefix, H, b / n_prefix, P_cap) * (d_head + 2) * sizeof(float);
 }
 
 extern "C" int shared_prefix_decode_attn(
@@ -1264,7 +1286,7 @@ extern "C" int shared_prefix_decode_attn(
   if (ws_bytes < sckv_shared_decode_workspace_bytes(b, H, n_prefix, P_cap, L_cap, d_head))
     return fail(SCKV_EINVAL, W + ": workspace too small");
   const size_t own = partial_bytes(b, H, L_cap, d_head);
-  const int n = prefix_chunks(dt == SCKV_BF16, n_prefix, H, b / n_prefix, P_cap);
+  const int n = prefix_chunks(dt == SCKV_BF16, d_head, n_prefix, H, b / n_prefix, P_cap);
   float* po = reinterpret_cast<float*>(static_cast<char*>(ws) + own);
   float* ml = po + (size_t)b * H * n * d_head;
   rc = launch_prefix(q, k_prefix, v_prefix, prefix_len, n_prefix, P_cap, cur_tok, pos ? pos : vu,

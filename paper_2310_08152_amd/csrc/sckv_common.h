@@ -29,7 +29,7 @@ int launch_move(void* kv, void* kv_out, int32_t M, int32_t b, int32_t H, int32_t
 // the part of shared_prefix_decode_attn that reads the prefixes (shared.hip):
 // n = prefix_chunks(...) partials a slice, outputs [slice][n][d] in log2 units
 // and (maximum, sum) [slice][n][2]
-int prefix_chunks(bool bf16, int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap);
+int prefix_chunks(bool bf16, int32_t d, int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap);
 int launch_prefix(const void* q, const void* k, const void* v, const int32_t* len,
                   int32_t n_prefix, int32_t P_cap, const int32_t* cur_tok, const int32_t* pos,
                   int32_t L_meta, int32_t b, int32_t H, int32_t d_head, sckv_dtype dt, float scale,

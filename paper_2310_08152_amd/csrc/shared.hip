@@ -4,7 +4,7 @@
 //
 // Per (prefix, head) the queries of its sequences form a matrix, so the scores
 // S^T = K Q^T and the outputs O^T += V^T P^T are products on the matrix cores.
-// A wave takes one tile of 32 queries and 32-row blocks of keys; lane l owns
+// A wave takes a tile of 32 queries (or two) and 32-row blocks of keys; lane l owns
 // query l % 32 of S^T (16 of the block's 32 rows: 8a + 4(l/32) + c), hence the
 // running maximum and sum of a softmax in registers, and the same rows of P^T
 // are the B operand of the value product as they stand.  bf16 queries are
@@ -39,7 +39,7 @@ struct PrefixFreq {
 // The 16 scores and weights of a lane, the wave's tile of queries and its
 // outputs.  DB blocks of 32 output elements; in each, register v of lane l
 // holds element 8 (v/4) + 4 (l/32) + v % 4 of query l % 32.
-template <typename T, int D>
+template <typename T, int D, int QT>
 struct PrefixTile {
   static constexpr int DB = (D + 31) / 32;
   static constexpr int KS = D / 16;
@@ -52,13 +52,13 @@ struct PrefixTile {
     u32x4 k[NK];
     uint32_t v[NV];
   };
-  bf16x8 qhi[sizeof(T) == 2 ? KS : 1], qlo[sizeof(T) == 2 ? KS : 1];
-  float qf[sizeof(T) == 2 ? 1 : D / 2];
-  f32x16 o[DB];
-  float M, l;
+  bf16x8 qhi[QT][sizeof(T) == 2 ? KS : 1], qlo[QT][sizeof(T) == 2 ? KS : 1];
+  float qf[QT][sizeof(T) == 2 ? 1 : D / 2];
+  f32x16 o[QT][DB];
+  float M[QT], l[QT];
 
-  // the lane's query, row `q` of D floats in LDS
-  __device__ __forceinline__ void take_query(const float* q, int h) {
+  // the lane's query of tile x, row `q` of D floats in LDS
+  __device__ __forceinline__ void take_query(int x, const float* q, int h) {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
@@ -69,21 +69,21 @@ struct PrefixTile {
           wh[i] = pack_bf16x2(x0, x1);
           wl[i] = pack_bf16x2(x0 - bf16_lo(wh[i]), x1 - bf16_hi(wh[i]));
         }
-        qhi[kk] = __builtin_bit_cast(bf16x8, wh);
-        qlo[kk] = __builtin_bit_cast(bf16x8, wl);
+        qhi[x][kk] = __builtin_bit_cast(bf16x8, wh);
+        qlo[x][kk] = __builtin_bit_cast(bf16x8, wl);
       }
     } else {
 #pragma unroll
       for (int p = 0; p < D / 8; ++p)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) qf[4 * p + j] = q[8 * p + 4 * h + j];
+        for (int j = 0; j < 4; ++j) qf[x][4 * p + j] = q[8 * p + 4 * h + j];
     }
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) o[b][v] = 0.f;
-    M = -INFINITY;
-    l = 0.f;
+      for (int v = 0; v < 16; ++v) o[x][b][v] = 0.f;
+    M[x] = -INFINITY;
+    l[x] = 0.f;
   }
 
   // Rows r .. r + 31 of a slice (those past `last` read row `last`).  bf16:
@@ -123,9 +123,11 @@ struct PrefixTile {
   // wave's own value tile in LDS
   __device__ __forceinline__ void step(const Rows& x, int r, int r1, float c, char* vt, int lane) {
     const int h = lane >> 5;
-    f32x16 s;
+    f32x16 s[QT];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = 0.f;
+    for (int q = 0; q < QT; ++q)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[q][v] = 0.f;
     if constexpr (sizeof(T) == 2) {
       // the values go to LDS row by row while the scores are multiplied (the
       // wave's own tile, and LDS serves a wave in order: no barrier)
@@ -137,53 +139,60 @@ struct PrefixTile {
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
         const bf16x8 k = __builtin_bit_cast(bf16x8, x.k[kk]);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qhi[kk], s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qlo[kk], s, 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < QT; ++q) s[q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qhi[q][kk], s[q], 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < QT; ++q) s[q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qlo[q][kk], s[q], 0, 0, 0);
       }
     } else {
 #pragma unroll
       for (int p = 0; p < D / 8; ++p)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.k[p][j]), qf[4 * p + j], s, 0, 0, 0);
+#pragma unroll
+          for (int q = 0; q < QT; ++q)
+            s[q] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.k[p][j]), qf[q][4 * p + j], s[q], 0, 0, 0);
     }
-    float mb = -INFINITY;
-    if (r + PRE_ROWS <= r1) {
+    if (r + PRE_ROWS > r1) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[v] *= c;
-        mb = fmaxf(mb, s[v]);
-      }
-    } else {
+      for (int q = 0; q < QT; ++q)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[v] = r + 8 * (v / 4) + 4 * h + v % 4 < r1 ? s[v] * c : -INFINITY;
-        mb = fmaxf(mb, s[v]);
-      }
+        for (int v = 0; v < 16; ++v) s[q][v] = r + 8 * (v / 4) + 4 * h + v % 4 < r1 ? s[q][v] : -INFINITY;
     }
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb), __float_as_uint(mb), false, false);
-    mb = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-    // finite in every lane from the first block on (its first row counts)
-    if (__any(mb > M + PRE_RESCALE)) {
-      const float mn = fmaxf(M, mb);
-      const float f = fast_exp2(M - mn);  // 0 while M = -inf
-      M = mn;
-      l *= f;
 #pragma unroll
-      for (int b = 0; b < DB; ++b)
+    for (int q = 0; q < QT; ++q) {
+      float mb = s[q][0];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[b][v] *= f;
+      for (int v = 1; v < 16; ++v) mb = fmaxf(mb, s[q][v]);
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mb), __float_as_uint(mb), false, false);
+      mb = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c;
+      // finite in every lane from the first block on (its first row counts)
+      if (__any(mb > M[q] + PRE_RESCALE)) {
+        const float mn = fmaxf(M[q], mb);
+        const float f = fast_exp2(M[q] - mn);  // 0 while M = -inf
+        M[q] = mn;
+        l[q] *= f;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[q][b][v] *= f;
+      }
     }
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        u32x4 p;
+        bf16x8 pb[QT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[i] = pack_bf16x2(fast_exp2(s[8 * t + 2 * i] - M), fast_exp2(s[8 * t + 2 * i + 1] - M));
-          l += bf16_lo(p[i]) + bf16_hi(p[i]);
+        for (int q = 0; q < QT; ++q) {
+          u32x4 p;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[i] = pack_bf16x2(fast_exp2(fmaf(s[q][8 * t + 2 * i], c, -M[q])),
+                               fast_exp2(fmaf(s[q][8 * t + 2 * i + 1], c, -M[q])));
+            l[q] += bf16_lo(p[i]) + bf16_hi(p[i]);
+          }
+          pb[q] = __builtin_bit_cast(bf16x8, p);
         }
-        const bf16x8 pb = __builtin_bit_cast(bf16x8, p);
         // V^T: elements 32 b + 16 (l/16 % 2) .. of rows 16 t + 8 j + 4 h + 0..3
         const int i16 = lane & 15;
         const char* at = vt + (16 * t + 4 * h + i16 / 4) * PITCH + 32 * ((lane >> 4) & 1) + 8 * (i16 % 4);
@@ -191,72 +200,77 @@ struct PrefixTile {
         for (int b = 0; b < DB; ++b) {
           const s16x4 lo = lds_read_tr16(at + 64 * b), hi = lds_read_tr16(at + 64 * b + 8 * PITCH);
           const s16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-          o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pb, o[b], 0, 0, 0);
+#pragma unroll
+          for (int q = 0; q < QT; ++q)
+            o[q][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pb[q], o[q][b], 0, 0, 0);
         }
       }
     } else {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const float p = fast_exp2(s[v] - M);
-        l += p;
 #pragma unroll
-        for (int b = 0; b < DB; ++b)
-          o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.v[v * DB + b]), p, o[b], 0, 0, 0);
+        for (int q = 0; q < QT; ++q) {
+          const float p = fast_exp2(fmaf(s[q][v], c, -M[q]));
+          l[q] += p;
+#pragma unroll
+          for (int b = 0; b < DB; ++b)
+            o[q][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.v[v * DB + b]), p, o[q][b], 0, 0, 0);
+        }
       }
     }
   }
-
-  // joins another wave's state of the same queries (LDS, [register][lane])
-  __device__ __forceinline__ void put(float* at, int lane) const {
-    at[lane] = M;
-    at[64 + lane] = l;
-#pragma unroll
-    for (int b = 0; b < DB; ++b)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) at[(2 + 16 * b + v) * 64 + lane] = o[b][v];
-  }
-  __device__ __forceinline__ void join(const float* at, int lane) {
-    const float m2 = at[lane], mn = fmaxf(M, m2);
-    const float f = M == -INFINITY ? 0.f : fast_exp2(M - mn);
-    const float g = m2 == -INFINITY ? 0.f : fast_exp2(m2 - mn);
-    M = mn;
-    l = l * f + at[64 + lane] * g;
-#pragma unroll
-    for (int b = 0; b < DB; ++b)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) o[b][v] = o[b][v] * f + at[(2 + 16 * b + v) * 64 + lane] * g;
-  }
-  static constexpr int STATE_BYTES = (2 + 16 * DB) * 64 * 4;
 };
 
-// one workgroup per (prefix, head, chunk of rows, NQ tiles of queries):
-// PRE_KEY_WAVES waves a tile
-template <typename T, int D, int NQ>
-__global__ __launch_bounds__(64 * PRE_KEY_WAVES * NQ, sizeof(T) == 2 ? 2 : 1) void prefix_kernel(
+// waves of a SIMD that the registers of a shape are held to
+constexpr int prefix_waves(bool bf16, int D, int QT) { return !bf16 ? 1 : D == 64 && QT == 1 ? 3 : 2; }
+
+// one workgroup per (prefix, head, chunk of rows, QT tiles of queries)
+template <typename T, int D, int QT>
+__global__ __launch_bounds__(64 * PRE_KEY_WAVES, prefix_waves(sizeof(T) == 2, D, QT)) void prefix_kernel(
     const T* __restrict__ q, const T* __restrict__ k_pre, const T* __restrict__ v_pre,
     const int32_t* __restrict__ pre_len, const int32_t* __restrict__ cur_tok,
     const int32_t* __restrict__ pos, int32_t L_meta, int32_t H, int32_t P_cap, int32_t per,
     int32_t n_chunk, int32_t n_slice, float c, int rotate, PrefixFreq tab, float* __restrict__ part_o,
     float2* __restrict__ part_ml) {
-  using Tile = PrefixTile<T, D>;
-  constexpr int THREADS = 64 * PRE_KEY_WAVES * NQ;
+  using Tile = PrefixTile<T, D, QT>;
+  constexpr int QUERIES = QT * PRE_QUERIES;
+  constexpr int THREADS = 64 * PRE_KEY_WAVES;
   constexpr int HD = D / 2;
+  constexpr int DB = Tile::DB;
   constexpr int QPITCH = D + 4;
-  constexpr int Q_BYTES = PRE_QUERIES * QPITCH * 4;
-  constexpr int TILE_BYTES = PRE_KEY_WAVES * Tile::V_BYTES;
-  constexpr int JOIN_BYTES = PRE_KEY_WAVES / 2 * Tile::STATE_BYTES;
-  constexpr int PER_TILE = std::max(std::max(Q_BYTES, TILE_BYTES), JOIN_BYTES);
-  __shared__ __align__(16) char lds[NQ * PER_TILE];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int tile = wave / PRE_KEY_WAVES, kw = wave % PRE_KEY_WAVES;
+  constexpr int Q_BYTES = QUERIES * QPITCH * 4;
+  constexpr int V_BYTES = PRE_KEY_WAVES * Tile::V_BYTES;
+  constexpr int O_BYTES = PRE_KEY_WAVES * 16 * DB * 64 * 4;
+  __shared__ __align__(16) char lds[std::max(std::max(Q_BYTES, V_BYTES), O_BYTES)];
+  __shared__ float2 meet[QT][PRE_KEY_WAVES][PRE_QUERIES];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int kw = __builtin_amdgcn_readfirstlane(tid >> 6);
   // chunks of a slice and slices first, tiles of queries behind: workgroups
   // that read the same rows are a multiple of the slices' chunks apart
   const int qt = blockIdx.x / (n_slice * n_chunk);
   const int rest = blockIdx.x - qt * (n_slice * n_chunk);
   const int slice = rest / n_chunk, chunk = rest - slice * n_chunk;
   const int g = slice / H, h_ = slice - g * H;
-  const int q0 = qt * NQ * PRE_QUERIES;  // first query of the workgroup (of the prefix's `per`)
+  const int q0 = qt * QUERIES;  // first query of the workgroup (of the prefix's `per`)
 
+  // The tile's queries, element pairs (e, e + d/2) by thread; every load is
+  // asked for before any is used (one pair after the other, with its token's
+  // position, the prologue took longer than 1000 rows).
+  constexpr int PAIRS = QUERIES * HD / THREADS;
+  static_assert(PAIRS * THREADS == QUERIES * HD, "whole pairs a thread");
+  T xr[PAIRS], yr[PAIRS];
+  int tok[PAIRS];
+  double freq[PAIRS];
+#pragma unroll
+  for (int i = 0; i < PAIRS; ++i) {
+    const int f = tid + i * THREADS, j = f / HD, e = f - j * HD;
+    const int s = g * per + min(q0 + j, per - 1);
+    const T* src = q + ((int64_t)s * H + h_) * D;
+    xr[i] = src[e];
+    yr[i] = src[e + HD];
+    tok[i] = rotate ? cur_tok[s] : 0;
+    freq[i] = rotate ? tab.w[e] : 0.0;
+  }
   const int n = min(max(pre_len[g], 0), P_cap);
   const int each = ((n + n_chunk - 1) / n_chunk + PRE_ROWS - 1) / PRE_ROWS * PRE_ROWS;
   const int r0 = min(chunk * (int64_t)each, (int64_t)n), r1 = min((int64_t)r0 + each, (int64_t)n);
@@ -266,48 +280,48 @@ __global__ __launch_bounds__(64 * PRE_KEY_WAVES * NQ, sizeof(T) == 2 ? 2 : 1) vo
   typename Tile::Rows A, B;
   constexpr int STRIDE = PRE_ROWS * PRE_KEY_WAVES;
   int r = r0 + PRE_ROWS * kw;
+  int ps[PAIRS];
+#pragma unroll
+  for (int i = 0; i < PAIRS; ++i) {
+    const int s = g * per + min(q0 + (tid + i * THREADS) / HD, per - 1);
+    // (a token outside the metadata: its step's output does not come from here)
+    ps[i] = rotate && tok[i] >= 0 && tok[i] < L_meta ? pos[(int64_t)s * L_meta + tok[i]] : 0;
+  }
   if (r < r1) Tile::load(A, kb, vb, r, r1 - 1, lane);
-
-  // the tile's queries, rotated, as floats in LDS
-  for (int i = tid; i < NQ * PRE_QUERIES * HD; i += THREADS) {
-    const int j = i / HD, e = i - j * HD;
-    const int s = g * per + q0 + j;
-    float x = 0.f, y = 0.f;
-    if (q0 + j < per) {
-      const T* src = q + ((int64_t)s * H + h_) * D;
-      if constexpr (sizeof(T) == 2) {
-        x = bf16_lo((uint32_t)src[e]);
-        y = bf16_lo((uint32_t)src[e + HD]);
-      } else {
-        x = src[e];
-        y = src[e + HD];
-      }
-      if (rotate) {
-        const int t = cur_tok[s];
-        // (a token outside the metadata: its step's output does not come from here)
-        const double ps = t >= 0 && t < L_meta ? (double)pos[(int64_t)s * L_meta + t] : 0.0;
-        const double two_pi = 6.283185307179586476925286766559;
-        const double inv_two_pi = 0.15915494309189533576888376337251;
-        double ang = ps * tab.w[e];
-        ang -= two_pi * rint(ang * inv_two_pi);
-        float sn, cs;
-        sincosf((float)ang, &sn, &cs);
-        const float x1 = x;
-        x = x1 * cs - y * sn;
-        y = y * cs + x1 * sn;
-      }
+#pragma unroll
+  for (int i = 0; i < PAIRS; ++i) {
+    const int f = tid + i * THREADS, j = f / HD, e = f - j * HD;
+    float x, y;
+    if constexpr (sizeof(T) == 2) {
+      x = bf16_lo((uint32_t)xr[i]);
+      y = bf16_lo((uint32_t)yr[i]);
+    } else {
+      x = xr[i];
+      y = yr[i];
     }
-    float* dst = reinterpret_cast<float*>(lds + j / PRE_QUERIES * PER_TILE) + j % PRE_QUERIES * QPITCH;
+    if (rotate) {
+      const double two_pi = 6.283185307179586476925286766559;
+      const double inv_two_pi = 0.15915494309189533576888376337251;
+      double ang = (double)ps[i] * freq[i];
+      ang -= two_pi * rint(ang * inv_two_pi);
+      float sn, cs;
+      sincosf((float)ang, &sn, &cs);
+      const float x1 = x;
+      x = x1 * cs - y * sn;
+      y = y * cs + x1 * sn;
+    }
+    float* dst = reinterpret_cast<float*>(lds) + j * QPITCH;
     dst[e] = x;
     dst[e + HD] = y;
   }
   __syncthreads();
-  char* mine = lds + tile * PER_TILE;
   Tile st;
-  st.take_query(reinterpret_cast<const float*>(mine) + (lane & 31) * QPITCH, lane >> 5);
+#pragma unroll
+  for (int x = 0; x < QT; ++x)
+    st.take_query(x, reinterpret_cast<const float*>(lds) + (PRE_QUERIES * x + (lane & 31)) * QPITCH, h);
   __syncthreads();  // every wave has its queries; the tiles of values take their place
 
-  char* vt = mine + kw * Tile::V_BYTES;
+  char* vt = lds + kw * Tile::V_BYTES;
   for (; r + 2 * STRIDE < r1; r += 2 * STRIDE) {
     Tile::load(B, kb, vb, r + STRIDE, r1 - 1, lane);
     st.step(A, r, r1, c, vt, lane);
@@ -321,48 +335,74 @@ __global__ __launch_bounds__(64 * PRE_KEY_WAVES * NQ, sizeof(T) == 2 ? 2 : 1) vo
     if (more) st.step(B, r + STRIDE, r1, c, vt, lane);
   }
 
-  // both halves of the wave hold a part of each query's sum
-  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.l), __float_as_uint(st.l), false, false);
-  st.l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  // the key waves' states meet pairwise in LDS
-  float* slots = reinterpret_cast<float*>(mine);
-  constexpr int SLOT = Tile::STATE_BYTES / 4;
-  __syncthreads();
-  if (kw >= 2) st.put(slots + (kw - 2) * SLOT, lane);
-  __syncthreads();
-  if (kw < 2) st.join(slots + kw * SLOT, lane);
-  __syncthreads();
-  if (kw == 1) st.put(slots, lane);
-  __syncthreads();
-  if (kw == 0) {
-    st.join(slots, lane);
-    const int j = q0 + tile * PRE_QUERIES + (lane & 31);
-    if (j < per) {
-      const int64_t p = (((int64_t)(g * per + j)) * H + h_) * n_chunk + chunk;
-      if (lane < 32) part_ml[p] = make_float2(st.M, st.l);
+  // The key waves meet: first their maxima and sums, then their outputs, each
+  // taken to the common maximum, of which every wave adds up a quarter (both
+  // halves of a wave hold a part of each query's sum).
 #pragma unroll
-      for (int b = 0; b < Tile::DB; ++b)
+  for (int x = 0; x < QT; ++x) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.l[x]), __float_as_uint(st.l[x]), false, false);
+    st.l[x] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (lane < 32) meet[x][kw][lane] = make_float2(st.M[x], st.l[x]);
+  }
+  __syncthreads();
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const int e = 32 * b + 8 * a + 4 * (lane >> 5);
-          if (e < D) {
-            const f32x4 w = {st.o[b][4 * a], st.o[b][4 * a + 1], st.o[b][4 * a + 2], st.o[b][4 * a + 3]};
-            *reinterpret_cast<f32x4*>(part_o + p * D + e) = w;
-          }
-        }
+  for (int x = 0; x < QT; ++x) {
+    float M = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < PRE_KEY_WAVES; ++w) M = fmaxf(M, meet[x][w][lane & 31].x);
+    const float m0 = M == -INFINITY ? 0.f : M;  // (no row at all)
+#pragma unroll
+    for (int w = 0; w < PRE_KEY_WAVES; ++w) {
+      const float2 y = meet[x][w][lane & 31];
+      l = fmaf(y.y, fast_exp2(y.x - m0), l);
     }
+    const float f = fast_exp2(st.M[x] - m0);  // 0 for a wave without rows
+    float* mine = reinterpret_cast<float*>(lds) + kw * 16 * DB * 64;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mine[(16 * b + v) * 64 + lane] = st.o[x][b][v] * f;
+    __syncthreads();
+    const int j = q0 + PRE_QUERIES * x + (lane & 31);
+    if (j < per) {
+      const int64_t p = ((int64_t)(g * per + j) * H + h_) * n_chunk + chunk;
+      if (tid < 32) part_ml[p] = make_float2(M, l);
+      // wave w: registers 4 w .. 4 w + 3 of each block, elements 32 b + 8 w + 4 h + 0..3
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        const int e = 32 * b + 8 * kw + 4 * h;
+        if (e >= D) continue;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < PRE_KEY_WAVES; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            sum[i] += reinterpret_cast<const float*>(lds)[((w * DB + b) * 16 + 4 * kw + i) * 64 + lane];
+        *reinterpret_cast<f32x4*>(part_o + p * D + e) = sum;
+      }
+    }
+    if (x + 1 < QT) __syncthreads();  // the next tile's outputs take their place
   }
 }
 
-// Chunks of each prefix slice: as many as give every CU its workgroups (two
-// of one tile, one of two tiles: about 220 registers a thread), none of less
-// than 128 rows.
-constexpr int PRE_FILL_WAVES = 2048;
-static int prefix_tiles(bool bf16, int32_t per) { return bf16 && per > PRE_QUERIES ? 2 : 1; }
-int prefix_chunks(bool bf16, int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap) {
-  const int nq = prefix_tiles(bf16, per);
-  const int64_t wgs = (int64_t)n_prefix * H * ((per + nq * PRE_QUERIES - 1) / (nq * PRE_QUERIES));
-  const int64_t want = std::max<int64_t>(1, PRE_FILL_WAVES / (PRE_KEY_WAVES * nq) / wgs);
+// Tiles of queries of a wave: two where it has them and holds both (bf16, 64
+// elements a head: 254 registers), so that each row is loaded once for 64
+// queries and two chains of softmax steps run beside each other (64 sequences
+// behind 12288 rows: the prefix's part 32.7 -> 25.6 us).  At 80 elements two
+// tiles leave one wave a SIMD, with the accumulators in the other half of the
+// registers (64 behind 4000 rows: 32 us with one tile, 37 with two).
+static int prefix_tiles(bool bf16, int32_t d, int32_t per) {
+  return bf16 && d == 64 && per > PRE_QUERIES ? 2 : 1;
+}
+// Chunks of each prefix slice: as many as give every CU a workgroup, none of
+// less than 128 rows.  Two workgroups a CU cost more at the ends (prologue,
+// partials) than they hide: 64 behind 12288 rows 48 and 52 us, 32 behind 4000
+// 20.6 and 21.5, 8 behind each of four of 2050 (80 elements) 28.8 and 28.2.
+constexpr int PRE_WGS = 256;
+int prefix_chunks(bool bf16, int32_t d, int32_t n_prefix, int32_t H, int32_t per, int32_t P_cap) {
+  const int q = prefix_tiles(bf16, d, per) * PRE_QUERIES;
+  const int64_t wgs = (int64_t)n_prefix * H * ((per + q - 1) / q);
+  const int64_t want = std::max<int64_t>(1, PRE_WGS / wgs);
   return (int)std::min<int64_t>(want, (P_cap + 127) / 128);
 }
 
@@ -373,25 +413,25 @@ static int launch_prefix_typed(const void* q, const void* k, const void* v, cons
                                float scale, float theta, float* part_o, float* part_ml,
                                hipStream_t stream) {
   const int per = b / n_prefix;
-  const int nq = prefix_tiles(sizeof(T) == 2, per);
-  const int qtiles = (per + nq * PRE_QUERIES - 1) / (nq * PRE_QUERIES);
-  const int nc = prefix_chunks(sizeof(T) == 2, n_prefix, H, per, P_cap);
+  const int q_wg = prefix_tiles(sizeof(T) == 2, D, per) * PRE_QUERIES;
+  const int qtiles = (per + q_wg - 1) / q_wg;
+  const int nc = prefix_chunks(sizeof(T) == 2, D, n_prefix, H, per, P_cap);
   const int64_t wgs = (int64_t)n_prefix * H * nc * qtiles;
   if (wgs > 0x7fffffff) return fail(SCKV_EUNSUP, "shared_prefix_decode_attn: too many slices");
   PrefixFreq tab;
   for (int i = 0; i < 40; ++i) tab.w[i] = 0.0;
   if (theta > 0.f)
     for (int i = 0; i < D / 2; ++i) tab.w[i] = std::pow((double)theta, -2.0 * i / D);
-  auto go = [&](auto kernel, int threads) {
-    kernel<<<(unsigned)wgs, threads, 0, stream>>>(
+  auto go = [&](auto kernel) {
+    kernel<<<(unsigned)wgs, 64 * PRE_KEY_WAVES, 0, stream>>>(
         static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), len, cur_tok,
         pos, L_meta, H, P_cap, per, nc, n_prefix * H, scale * 1.4426950408889634f, theta > 0.f, tab,
         part_o, reinterpret_cast<float2*>(part_ml));
-    return hip_check(hipGetLastError(), "shared_prefix_decode_attn: prefix launch");
   };
-  if constexpr (sizeof(T) == 2)
-    if (nq == 2) return go(prefix_kernel<T, D, 2>, 128 * PRE_KEY_WAVES);
-  return go(prefix_kernel<T, D, 1>, 64 * PRE_KEY_WAVES);
+  constexpr int MOST = sizeof(T) == 2 && D == 64 ? 2 : 1;
+  if (q_wg > PRE_QUERIES) go(prefix_kernel<T, D, MOST>);
+  else go(prefix_kernel<T, D, 1>);
+  return hip_check(hipGetLastError(), "shared_prefix_decode_attn: prefix launch");
 }
 
 int launch_prefix(const void* q, const void* k, const void* v, const int32_t* len,
