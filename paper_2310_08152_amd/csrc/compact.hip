@@ -145,10 +145,29 @@ __device__ int first_moving_rank(const int32_t* __restrict__ ks, int n, int* sh)
   return t1 == 0x7fffffff ? n : t0 * S + t1;
 }
 
-template <int ROWB, int U>
+// accumulated weights that move with the rows: n_kv slices of the cache, then
+// those of the weights
+struct MoveRows {
+  static constexpr bool WEIGHTS = false;
+};
+struct MoveWeights {
+  static constexpr bool WEIGHTS = true;
+  const float* w;
+  float* w_out;
+  int32_t n_kv;
+};
+
+template <int ROWB, int U, typename X>
 __global__ __launch_bounds__(MOVE_THREADS) void compact_move_kernel(
     char* kv, char* kv_out, int32_t b, int32_t H, int32_t L_cap,
-    const int32_t* __restrict__ kv_len, const int32_t* __restrict__ kept_src) {
+    const int32_t* __restrict__ kv_len, const int32_t* __restrict__ kept_src, X x) {
+  if constexpr (X::WEIGHTS) {
+    static_assert(MOVE_THREADS == WMOVE_THREADS, "one launch");
+    if ((int)blockIdx.x >= x.n_kv) {
+      move_weights(x.w, x.w_out, (int)blockIdx.x - x.n_kv, b, H, L_cap, kv_len, kept_src);
+      return;
+    }
+  }
   constexpr int PPR = ROWB / 16;  // 16-byte pieces per row
   __shared__ int sh[MOVE_THREADS / 64];
   const int64_t slice = blockIdx.x;
@@ -185,19 +204,26 @@ __global__ __launch_bounds__(MOVE_THREADS) void compact_move_kernel(
 
 int launch_move(void* kv, void* kv_out, int32_t M, int32_t b, int32_t H, int32_t L_cap,
                 int32_t d_head, sckv_dtype dt, const int32_t* kv_len, const int32_t* kept_src,
-                const char* what, hipStream_t stream) {
+                const char* what, hipStream_t stream, const float* w, float* w_out) {
   const int rowb = d_head * elem_bytes(dt);
   char* a = static_cast<char*>(kv);
   char* o = static_cast<char*>(kv_out);
-  const unsigned g = (unsigned)((int64_t)M * 2 * b * H);
+  const int64_t n_kv = (int64_t)M * 2 * b * H;
+  auto go = [&](auto kernel, auto x, int64_t n) {
+    kernel<<<(unsigned)n, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src, x);
+    return hip_check(hipGetLastError(), what);
+  };
+#define SCKV_MOVE(ROWB)                                                                             \
+  (w ? go(compact_move_kernel<ROWB, 8, MoveWeights>, MoveWeights{w, w_out, (int32_t)n_kv}, n_kv / 2 * 3) \
+     : go(compact_move_kernel<ROWB, 8, MoveRows>, MoveRows{}, n_kv))
   switch (rowb) {
-    case 128: compact_move_kernel<128, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src); break;
-    case 160: compact_move_kernel<160, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src); break;
-    case 256: compact_move_kernel<256, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src); break;
-    case 320: compact_move_kernel<320, 8><<<g, MOVE_THREADS, 0, stream>>>(a, o, b, H, L_cap, kv_len, kept_src); break;
+    case 128: return SCKV_MOVE(128);
+    case 160: return SCKV_MOVE(160);
+    case 256: return SCKV_MOVE(256);
+    case 320: return SCKV_MOVE(320);
     default: return fail(SCKV_EUNSUP, std::string(what) + ": unsupported row size");
   }
-  return hip_check(hipGetLastError(), what);
+#undef SCKV_MOVE
 }
 
 }  // namespace sckv

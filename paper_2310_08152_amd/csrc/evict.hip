@@ -11,8 +11,8 @@
 //            searches), then a stable scan over the rows as in the compaction,
 //            with rows equal to that total taken from the lowest on (2048 rows:
 //            9 us; 31 where one thread searched the counts).
-//   move   : the compaction's mover for the cache; one workgroup per slice for
-//            the weights.
+//   move   : the compaction's mover, with one more workgroup per slice of
+//            weights.
 #include "sckv_common.h"
 
 namespace sckv {
@@ -174,46 +174,10 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(
   if (tid == 0) kv_len[s] = kept;
 }
 
-constexpr int WMOVE_THREADS = 256;
-constexpr int WMOVE_U = 4;
-
 __global__ __launch_bounds__(WMOVE_THREADS) void move_weights_kernel(
     const float* w, float* w_out, int32_t b, int32_t H, int32_t L_cap,
     const int32_t* __restrict__ kv_len, const int32_t* __restrict__ kept_src) {
-  const int64_t slice = blockIdx.x;
-  const int s = (int)((slice / H) % b);
-  const int n = min(max(kv_len[s], 0), L_cap);
-  const int32_t* ks = kept_src + (int64_t)s * L_cap;
-  const float* src = w + slice * L_cap;
-  float* dst = w_out + slice * L_cap;
-  // rows only move up (ks[r] >= r): chunks in ascending order, each read whole
-  // before it is written, never overwrite a row still to be read
-  for (int base = 0; base < n; base += WMOVE_THREADS * WMOVE_U) {
-    float v[WMOVE_U];
-#pragma unroll
-    for (int u = 0; u < WMOVE_U; ++u) {
-      const int r = base + u * WMOVE_THREADS + threadIdx.x;
-      int from = r < n ? ks[r] : -1;
-      v[u] = from >= 0 && from < L_cap ? src[from] : 0.f;
-    }
-    wait_vmem();
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < WMOVE_U; ++u) {
-      const int r = base + u * WMOVE_THREADS + threadIdx.x;
-      if (r < n) dst[r] = v[u];
-    }
-  }
-  __syncthreads();  // the last chunk's rows have been read
-  for (int r = n + threadIdx.x; r < L_cap; r += WMOVE_THREADS) dst[r] = 0.f;
-}
-
-static int launch_move_weights(const float* w, float* w_out, int64_t slices, int32_t b, int32_t H,
-                               int32_t L_cap, const int32_t* kv_len, const int32_t* kept_src,
-                               const char* what, hipStream_t stream) {
-  move_weights_kernel<<<(unsigned)slices, WMOVE_THREADS, 0, stream>>>(w, w_out, b, H, L_cap, kv_len,
-                                                                      kept_src);
-  return hip_check(hipGetLastError(), what);
+  move_weights(w, w_out, blockIdx.x, b, H, L_cap, kv_len, kept_src);
 }
 
 }  // namespace sckv
@@ -232,8 +196,9 @@ extern "C" int kv_compact_weights(float* w, float* w_out, int32_t M, int32_t b, 
     return fail(SCKV_EINVAL, "kv_compact_weights: w and w_out must be 4-byte aligned");
   const int64_t slices = (int64_t)M * b * H;
   if (slices > 0x7fffffff) return fail(SCKV_EUNSUP, "kv_compact_weights: too many slices");
-  return launch_move_weights(w, w_out ? w_out : w, slices, b, H, L_cap, kv_len, kept_src_row,
-                             "kv_compact_weights: launch", stream);
+  move_weights_kernel<<<(unsigned)slices, WMOVE_THREADS, 0, stream>>>(w, w_out ? w_out : w, b, H, L_cap,
+                                                                      kv_len, kept_src_row);
+  return hip_check(hipGetLastError(), "kv_compact_weights: launch");
 }
 
 extern "C" int kv_evict(void* kv, void* kv_out, float* w, float* w_out, int32_t M, int32_t b,
@@ -255,7 +220,7 @@ extern "C" int kv_evict(void* kv, void* kv_out, float* w, float* w_out, int32_t 
   if (!aligned16(kv) || (kv_out && !aligned16(kv_out)) || !aligned4(w) || !aligned4(w_out))
     return fail(SCKV_EINVAL, "kv_evict: buffers must be 16-byte aligned");
   const int64_t slices = (int64_t)M * b * H;
-  if (2 * slices > 0x7fffffff) return fail(SCKV_EUNSUP, "kv_evict: too many slices");
+  if (3 * slices > 0x7fffffff) return fail(SCKV_EUNSUP, "kv_evict: too many slices");
   const dim3 grid((unsigned)((L_cap + SUM_ROWS - 1) / SUM_ROWS), (unsigned)(b < 65535 ? b : 65535));
   evict_total_kernel<<<grid, 64 * SUM_WAVES, 0, stream>>>(w, M * H, b, H, make_div((uint32_t)H), L_cap,
                                                           kv_len, total);
@@ -265,9 +230,6 @@ extern "C" int kv_evict(void* kv, void* kv_out, float* w, float* w_out, int32_t 
                                                      recent, kept_src_row);
   rc = hip_check(hipGetLastError(), "kv_evict: select launch");
   if (rc) return rc;
-  rc = launch_move(kv, kv_out, M, b, H, L_cap, d_head, dt, kv_len, kept_src_row,
-                   "kv_evict: move launch", stream);
-  if (rc) return rc;
-  return launch_move_weights(w, w_out ? w_out : w, slices, b, H, L_cap, kv_len, kept_src_row,
-                             "kv_evict: weights launch", stream);
+  return launch_move(kv, kv_out, M, b, H, L_cap, d_head, dt, kv_len, kept_src_row, "kv_evict: move launch",
+                     stream, w, w_out ? w_out : w);
 }

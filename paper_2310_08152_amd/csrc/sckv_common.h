@@ -20,11 +20,12 @@ void clear_error();
 int fail(int code, const std::string& msg);
 int hip_check(hipError_t e, const char* what);
 
-// moves the rows that kept_src lists to the front of every cache slice
-// (compact.hip); kv_out null: in place
+// moves the rows that kept_src lists to the front of every cache slice, and
+// with w the accumulated weights alike (compact.hip); kv_out null: in place
 int launch_move(void* kv, void* kv_out, int32_t M, int32_t b, int32_t H, int32_t L_cap,
                 int32_t d_head, sckv_dtype dt, const int32_t* kv_len, const int32_t* kept_src,
-                const char* what, hipStream_t stream);
+                const char* what, hipStream_t stream, const float* w = nullptr,
+                float* w_out = nullptr);
 
 // the part of shared_prefix_decode_attn that reads the prefixes (shared.hip):
 // n = prefix_chunks(...) partials a slice, outputs [slice][n][d] in log2 units
@@ -241,6 +242,40 @@ constexpr int half_wave_count() {
   if constexpr (MASK == 0) return NV;
   else if constexpr (NV % 2 == 0) return half_wave_count<NV / 2, MASK / 2>();
   else return half_wave_count<NV, MASK / 2>();
+}
+
+// Moves one slice's accumulated weights as kept_src says and clears those
+// behind.  Rows only move up (kept_src[r] >= r): chunks in ascending order, each
+// read whole before it is written, never overwrite a row still to be read.
+constexpr int WMOVE_THREADS = 256;
+constexpr int WMOVE_U = 4;
+__device__ __forceinline__ void move_weights(const float* w, float* w_out, int64_t slice, int32_t b,
+                                             int32_t H, int32_t L_cap,
+                                             const int32_t* __restrict__ kv_len,
+                                             const int32_t* __restrict__ kept_src) {
+  const int s = (int)((slice / H) % b);
+  const int n = min(max(kv_len[s], 0), L_cap);
+  const int32_t* ks = kept_src + (int64_t)s * L_cap;
+  const float* src = w + slice * L_cap;
+  float* dst = w_out + slice * L_cap;
+  for (int base = 0; base < n; base += WMOVE_THREADS * WMOVE_U) {
+    float v[WMOVE_U];
+#pragma unroll
+    for (int u = 0; u < WMOVE_U; ++u) {
+      const int r = base + u * WMOVE_THREADS + threadIdx.x;
+      const int from = r < n ? ks[r] : -1;
+      v[u] = from >= 0 && from < L_cap ? src[from] : 0.f;
+    }
+    wait_vmem();
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < WMOVE_U; ++u) {
+      const int r = base + u * WMOVE_THREADS + threadIdx.x;
+      if (r < n) dst[r] = v[u];
+    }
+  }
+  __syncthreads();  // the last chunk's rows have been read
+  for (int r = n + threadIdx.x; r < L_cap; r += WMOVE_THREADS) dst[r] = 0.f;
 }
 
 __device__ __forceinline__ int lane_id() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)); }

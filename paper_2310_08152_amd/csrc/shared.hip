@@ -7,11 +7,12 @@
 // A wave takes a tile of 32 queries (or two) and 32-row blocks of keys; lane l owns
 // query l % 32 of S^T (16 of the block's 32 rows: 8a + 4(l/32) + c), hence the
 // running maximum and sum of a softmax in registers, and the same rows of P^T
-// are the B operand of the value product as they stand.  bf16 queries are
-// carried as two bf16 terms after the rotation (2^-17 of a score, as in the
-// decode step); the softmax weights are rounded to bf16 for the value product
-// (half a step of the output's own type a weight, averaged over the rows) and
-// their sum is that of the rounded ones.
+// are the B operand of the value product as they stand.  bf16 queries (after
+// the rotation) and softmax weights are carried as two bf16 terms each (2^-17
+// of them), so that a shared step is as exact as a decode step, which weighs
+// in fp32; weights of one term cost half a step of the output's own type and
+// saved 2% (64 sequences behind 12288 rows) or nothing (32 and fewer, bound by
+// HBM).
 //
 // Bound by HBM while a tile of queries is not much larger than the card's
 // flops per byte; the workgroup's four key waves split its rows, and the rows
@@ -47,11 +48,14 @@ struct PrefixTile {
                                      // reads' 8 rows x 64 bytes then meet no bank twice
   static constexpr int V_BYTES = sizeof(T) == 2 ? PRE_ROWS * PITCH : 0;
   static constexpr int NK = sizeof(T) == 2 ? KS : D / 8;   // 16-byte pieces of a key row per lane
-  static constexpr int NV = sizeof(T) == 2 ? KS * 4 : 16 * DB;  // registers of a block's values
+  // A block's rows in registers, loaded a block ahead.  bf16 values pass
+  // through LDS at the start of their block's step, so one set of them (`v`) is
+  // enough, refilled at once.
   struct Rows {
     u32x4 k[NK];
-    uint32_t v[NV];
+    float v[sizeof(T) == 2 ? 1 : 16 * DB];
   };
+  u32x4 v[sizeof(T) == 2 ? KS : 1];
   bf16x8 qhi[QT][sizeof(T) == 2 ? KS : 1], qlo[QT][sizeof(T) == 2 ? KS : 1];
   float qf[QT][sizeof(T) == 2 ? 1 : D / 2];
   f32x16 o[QT][DB];
@@ -96,15 +100,8 @@ struct PrefixTile {
     const int64_t row = min(r + (lane & 31), last);
     if constexpr (sizeof(T) == 2) {
       const T* kp = kb + row * D + 8 * h;
-      const T* vp = vb + row * D + 8 * h;
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) x.k[kk] = ld16(kp + 16 * kk);
-#pragma unroll
-      for (int kk = 0; kk < KS; ++kk) {
-        const u32x4 w = ld16(vp + 16 * kk);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x.v[4 * kk + i] = w[i];
-      }
     } else {
       const T* kp = kb + row * D + 4 * h;
 #pragma unroll
@@ -114,14 +111,22 @@ struct PrefixTile {
         const T* vp = vb + (int64_t)min(r + 8 * (v / 4) + 4 * h + v % 4, last) * D;
 #pragma unroll
         for (int b = 0; b < DB; ++b)  // (elements past the head size are never stored)
-          x.v[v * DB + b] = __float_as_uint(vp[min(32 * b + (lane & 31), D - 1)]);
+          x.v[v * DB + b] = vp[min(32 * b + (lane & 31), D - 1)];
       }
+    }
+  }
+  __device__ __forceinline__ void load_values(const T* vb, int r, int last, int lane) {
+    if constexpr (sizeof(T) == 2) {
+      const T* vp = vb + (int64_t)min(r + (lane & 31), last) * D + 8 * (lane >> 5);
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) v[kk] = ld16(vp + 16 * kk);
     }
   }
 
   // one block of rows r .. r + 31, of which those before r1 count; vt is the
-  // wave's own value tile in LDS
-  __device__ __forceinline__ void step(const Rows& x, int r, int r1, float c, char* vt, int lane) {
+  // wave's own value tile in LDS; the wave's next block starts at row `after`
+  __device__ __forceinline__ void step(const Rows& x, const T* vb, int r, int after, int r1, float c,
+                                       char* vt, int lane) {
     const int h = lane >> 5;
     f32x16 s[QT];
 #pragma unroll
@@ -132,10 +137,8 @@ struct PrefixTile {
       // the values go to LDS row by row while the scores are multiplied (the
       // wave's own tile, and LDS serves a wave in order: no barrier)
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk) {
-        const u32x4 w = {x.v[4 * kk], x.v[4 * kk + 1], x.v[4 * kk + 2], x.v[4 * kk + 3]};
-        st16(vt + (lane & 31) * PITCH + 32 * kk + 16 * h, w);
-      }
+      for (int kk = 0; kk < KS; ++kk) st16(vt + (lane & 31) * PITCH + 32 * kk + 16 * h, v[kk]);
+      if (after < r1) load_values(vb, after, r1 - 1, lane);
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
         const bf16x8 k = __builtin_bit_cast(bf16x8, x.k[kk]);
@@ -181,17 +184,20 @@ struct PrefixTile {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        bf16x8 pb[QT];
+        bf16x8 pb[QT], pl[QT];
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-          u32x4 p;
+          u32x4 p, e;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            p[i] = pack_bf16x2(fast_exp2(fmaf(s[q][8 * t + 2 * i], c, -M[q])),
-                               fast_exp2(fmaf(s[q][8 * t + 2 * i + 1], c, -M[q])));
-            l[q] += bf16_lo(p[i]) + bf16_hi(p[i]);
+            const float p0 = fast_exp2(fmaf(s[q][8 * t + 2 * i], c, -M[q]));
+            const float p1 = fast_exp2(fmaf(s[q][8 * t + 2 * i + 1], c, -M[q]));
+            p[i] = pack_bf16x2(p0, p1);
+            e[i] = pack_bf16x2(p0 - bf16_lo(p[i]), p1 - bf16_hi(p[i]));
+            l[q] += p0 + p1;
           }
           pb[q] = __builtin_bit_cast(bf16x8, p);
+          pl[q] = __builtin_bit_cast(bf16x8, e);
         }
         // V^T: elements 32 b + 16 (l/16 % 2) .. of rows 16 t + 8 j + 4 h + 0..3
         const int i16 = lane & 15;
@@ -203,6 +209,9 @@ struct PrefixTile {
 #pragma unroll
           for (int q = 0; q < QT; ++q)
             o[q][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pb[q], o[q][b], 0, 0, 0);
+#pragma unroll
+          for (int q = 0; q < QT; ++q)
+            o[q][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pl[q], o[q][b], 0, 0, 0);
         }
       }
     } else {
@@ -214,7 +223,7 @@ struct PrefixTile {
           l[q] += p;
 #pragma unroll
           for (int b = 0; b < DB; ++b)
-            o[q][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.v[v * DB + b]), p, o[q][b], 0, 0, 0);
+            o[q][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.v[v * DB + b], p, o[q][b], 0, 0, 0);
         }
       }
     }
@@ -287,7 +296,11 @@ __global__ __launch_bounds__(64 * PRE_KEY_WAVES, prefix_waves(sizeof(T) == 2, D,
     // (a token outside the metadata: its step's output does not come from here)
     ps[i] = rotate && tok[i] >= 0 && tok[i] < L_meta ? pos[(int64_t)s * L_meta + tok[i]] : 0;
   }
-  if (r < r1) Tile::load(A, kb, vb, r, r1 - 1, lane);
+  Tile st;
+  if (r < r1) {
+    Tile::load(A, kb, vb, r, r1 - 1, lane);
+    st.load_values(vb, r, r1 - 1, lane);
+  }
 #pragma unroll
   for (int i = 0; i < PAIRS; ++i) {
     const int f = tid + i * THREADS, j = f / HD, e = f - j * HD;
@@ -315,7 +328,6 @@ __global__ __launch_bounds__(64 * PRE_KEY_WAVES, prefix_waves(sizeof(T) == 2, D,
     dst[e + HD] = y;
   }
   __syncthreads();
-  Tile st;
 #pragma unroll
   for (int x = 0; x < QT; ++x)
     st.take_query(x, reinterpret_cast<const float*>(lds) + (PRE_QUERIES * x + (lane & 31)) * QPITCH, h);
@@ -324,15 +336,15 @@ __global__ __launch_bounds__(64 * PRE_KEY_WAVES, prefix_waves(sizeof(T) == 2, D,
   char* vt = lds + kw * Tile::V_BYTES;
   for (; r + 2 * STRIDE < r1; r += 2 * STRIDE) {
     Tile::load(B, kb, vb, r + STRIDE, r1 - 1, lane);
-    st.step(A, r, r1, c, vt, lane);
+    st.step(A, vb, r, r + STRIDE, r1, c, vt, lane);
     Tile::load(A, kb, vb, r + 2 * STRIDE, r1 - 1, lane);
-    st.step(B, r + STRIDE, r1, c, vt, lane);
+    st.step(B, vb, r + STRIDE, r + 2 * STRIDE, r1, c, vt, lane);
   }
   if (r < r1) {
     const bool more = r + STRIDE < r1;
     if (more) Tile::load(B, kb, vb, r + STRIDE, r1 - 1, lane);
-    st.step(A, r, r1, c, vt, lane);
-    if (more) st.step(B, r + STRIDE, r1, c, vt, lane);
+    st.step(A, vb, r, r + STRIDE, r1, c, vt, lane);
+    if (more) st.step(B, vb, r + STRIDE, r1, r1, c, vt, lane);
   }
 
   // The key waves meet: first their maxima and sums, then their outputs, each
@@ -388,7 +400,7 @@ __global__ __launch_bounds__(64 * PRE_KEY_WAVES, prefix_waves(sizeof(T) == 2, D,
 // Tiles of queries of a wave: two where it has them and holds both (bf16, 64
 // elements a head: 254 registers), so that each row is loaded once for 64
 // queries and two chains of softmax steps run beside each other (64 sequences
-// behind 12288 rows: the prefix's part 32.7 -> 25.6 us).  At 80 elements two
+// behind 12288 rows: the prefix's part 32.7 -> 25.9 us).  At 80 elements two
 // tiles leave one wave a SIMD, with the accumulators in the other half of the
 // registers (64 behind 4000 rows: 32 us with one tile, 37 with two).
 static int prefix_tiles(bool bf16, int32_t d, int32_t per) {

@@ -70,11 +70,10 @@ class Shared:
                         v[:, None]], 1)
         ow, _, A, pv = R.attend(q, ks, vs, d ** -0.5)
         # scores as in a decode step; bf16: the prefix's softmax weights are
-        # rounded to bf16 for the value product (half a step each), and their
-        # sum is that of the rounded ones
+        # two bf16 terms in the value product (2^-17 of a weight at most)
         bf = dt == torch.bfloat16
         rel = 2 * A * ((d + 24) * R.U + (2.0 ** -17 if bf else 0)) + (m + n + 64) * R.U
-        rel += 2 * R.half_step(dt) if bf else 0
+        rel += 2.0 ** -17 if bf else 0
         err = (self.o[s].double().cpu() - ow).abs()
         assert bool((err <= pv * rel + R.half_step(dt) * (ow.abs() + pv * rel)).all()), \
             (s, float(err.max()), float(err.max() / pv.max()))
