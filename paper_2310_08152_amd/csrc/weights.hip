@@ -46,14 +46,23 @@ struct TileSum {
 struct WeightPlan {
   int32_t *row, *tok, *vu;  // [b][entries]
   TileSum* sum;             // [b][entries / W_TILE]
-  int2* tiles;              // [b]: tiles that some query sees, all tiles
-  int32_t entries;
+  int32_t* tiles;           // [b]: tiles listed
+  int32_t entries;          // of a sequence
+  int32_t chunk;            // of each PLAN_CHUNK rows
 };
 
-// entries of a sequence's list: every row, and each class up to W_CLASS - 1 more
-static int64_t plan_entries(int32_t L_cap) {
-  return ((int64_t)L_cap + W_CLASS - 1) / W_CLASS * W_CLASS + 3 * W_CLASS;
+constexpr int PLAN_WAVES = 16;
+constexpr int PLAN_THREADS = 64 * PLAN_WAVES;
+constexpr int PLAN_U = 4;  // rows of a thread, in flight together
+constexpr int PLAN_CHUNK = PLAN_THREADS * PLAN_U;
+
+// Entries of a sequence's list.  Each PLAN_CHUNK rows have a part of their own
+// (a workgroup plans it): every row, and each class up to W_CLASS - 1 more.
+static int32_t chunk_entries(int32_t L_cap) {
+  return (std::min(L_cap, PLAN_CHUNK) + W_CLASS - 1) / W_CLASS * W_CLASS + 3 * W_CLASS;
 }
+static int32_t plan_chunks(int32_t L_cap) { return (L_cap + PLAN_CHUNK - 1) / PLAN_CHUNK; }
+static int64_t plan_entries(int32_t L_cap) { return (int64_t)plan_chunks(L_cap) * chunk_entries(L_cap); }
 static size_t plan_bytes(int32_t b, int32_t L_cap) {
   const size_t e = (size_t)plan_entries(L_cap);
   return (size_t)b * (3 * e * 4 + e / W_TILE * sizeof(TileSum) + 16);
@@ -62,121 +71,94 @@ static WeightPlan plan_at(void* ws, int32_t b, int32_t L_cap) {
   const size_t e = (size_t)plan_entries(L_cap);
   WeightPlan p;
   p.entries = (int32_t)e;
+  p.chunk = chunk_entries(L_cap);
   p.row = static_cast<int32_t*>(ws);
   p.tok = p.row + (size_t)b * e;
   p.vu = p.tok + (size_t)b * e;
   p.sum = reinterpret_cast<TileSum*>(p.vu + (size_t)b * e);
-  p.tiles = reinterpret_cast<int2*>(p.sum + (size_t)b * (e / W_TILE));
+  p.tiles = reinterpret_cast<int32_t*>(p.sum + (size_t)b * (e / W_TILE));
   return p;
 }
 
-constexpr int PLAN_WAVES = 16;
-constexpr int PLAN_U = 4;  // rows of a thread in flight
-constexpr int PLAN_THREADS = 64 * PLAN_WAVES;
-
+// one workgroup per chunk of a sequence
 __global__ __launch_bounds__(PLAN_THREADS) void weight_plan_kernel(
     WeightPlan p, const int32_t* __restrict__ vu, int32_t L_meta, int32_t tok0, int32_t nq,
-    const int32_t* __restrict__ kv_len, const int32_t* __restrict__ tok_idx, int32_t L_cap) {
-  constexpr int CHUNK = PLAN_THREADS * PLAN_U;
+    const int32_t* __restrict__ kv_len, const int32_t* __restrict__ tok_idx, int32_t L_cap,
+    int32_t chunks) {
   static_assert(PLAN_U * PLAN_WAVES == 64, "one wave scans the counts of a class");
   // rows of class k that pass u of wave w holds, then those before them, at
-  // [k][u * PLAN_WAVES + w]; the chunk's total behind them
+  // [k][u * PLAN_WAVES + w]; the total behind them
   __shared__ int before[3][65];
-  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n = min(max(kv_len[s], 0), L_cap);
-  const int32_t* toks = tok_idx + (int64_t)s * L_cap;
+  const int s = blockIdx.x / chunks, chunk = blockIdx.x - s * chunks;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int held = min(max(kv_len[s], 0), L_cap);
+  if (chunk == 0 && tid == 0)
+    p.tiles[s] = (held + PLAN_CHUNK - 1) / PLAN_CHUNK * (p.chunk / W_TILE);
+  const int row0 = chunk * PLAN_CHUNK;
+  const int n = min(held - row0, PLAN_CHUNK);  // rows of this chunk
+  if (n <= 0) return;
+  const int32_t* toks = tok_idx + (int64_t)s * L_cap + row0;
   const int32_t* vus = vu + (int64_t)s * L_meta;
-  const int64_t at = (int64_t)s * p.entries;
+  const int64_t at = (int64_t)s * p.entries + (int64_t)chunk * p.chunk;
   const int last = tok0 + nq - 1;  // last query's token
   // classes: 0 seen by every later query, 1 by some, 2 by none (3: no row)
   int j[PLAN_U], v[PLAN_U], c[PLAN_U];
   uint64_t m[3][PLAN_U];
-  auto classify = [&](int base) {
 #pragma unroll
-    for (int u = 0; u < PLAN_U; ++u) j[u] = toks[min(base + u * PLAN_THREADS + tid, n - 1)];
+  for (int u = 0; u < PLAN_U; ++u) j[u] = toks[min(u * PLAN_THREADS + tid, n - 1)];
 #pragma unroll
-    for (int u = 0; u < PLAN_U; ++u) v[u] = vus[min(max(j[u], 0), L_meta - 1)];
+  for (int u = 0; u < PLAN_U; ++u) v[u] = vus[min(max(j[u], 0), L_meta - 1)];
 #pragma unroll
-    for (int u = 0; u < PLAN_U; ++u) {
-      const bool none = j[u] < 0 || j[u] >= L_meta || v[u] == j[u] || j[u] > last || v[u] < tok0 || nq == 0;
-      c[u] = base + u * PLAN_THREADS + tid >= n ? 3 : none ? 2 : v[u] >= last ? 0 : 1;
+  for (int u = 0; u < PLAN_U; ++u) {
+    const bool none = j[u] < 0 || j[u] >= L_meta || v[u] == j[u] || j[u] > last || v[u] < tok0 || nq == 0;
+    c[u] = u * PLAN_THREADS + tid >= n ? 3 : none ? 2 : v[u] >= last ? 0 : 1;
 #pragma unroll
-      for (int k = 0; k < 3; ++k) m[k][u] = __ballot(c[u] == k);
-    }
-  };
-  // a chunk's counts become exclusive prefix sums
-  auto scan = [&]() {
-    __syncthreads();  // those of the chunk before have been read
-#pragma unroll
-    for (int u = 0; u < PLAN_U; ++u) {
-      const int x0 = __popcll(m[0][u]), x1 = __popcll(m[1][u]), x2 = __popcll(m[2][u]);
-      if (lane < 3) before[lane][u * PLAN_WAVES + wave] = lane == 0 ? x0 : lane == 1 ? x1 : x2;
-    }
-    __syncthreads();
-    if (wave < 3) {
-      const int x = before[wave][lane];
-      int sum = x;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(sum, off, 64);
-        if (lane >= off) sum += y;
-      }
-      before[wave][lane] = sum - x;
-      if (lane == 63) before[wave][64] = sum;
-    }
-    __syncthreads();
-  };
-  // rows of each class
-  int total[3] = {0, 0, 0};
-  for (int base = 0; base < n; base += CHUNK) {
-    classify(base);
-    scan();
-#pragma unroll
-    for (int k = 0; k < 3; ++k) total[k] += before[k][64];
+    for (int k = 0; k < 3; ++k) m[k][u] = __ballot(c[u] == k);
+    const int x0 = __popcll(m[0][u]), x1 = __popcll(m[1][u]), x2 = __popcll(m[2][u]);
+    if (lane < 3) before[lane][u * PLAN_WAVES + wave] = lane == 0 ? x0 : lane == 1 ? x1 : x2;
   }
-  int start = 0, first[3], done[3];
+  __syncthreads();
+  if (wave < 3) {  // the counts become exclusive prefix sums
+    const int x = before[wave][lane];
+    int sum = x;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(sum, off, 64);
+      if (lane >= off) sum += y;
+    }
+    before[wave][lane] = sum - x;
+    if (lane == 63) before[wave][64] = sum;
+  }
+  __syncthreads();
+  // the rows, in order within each class; what is left of a class's last tiles
+  // and of the chunk's part is row -1, seen by none
+  int start = 0;
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    first[k] = done[k] = start;
-    start += (total[k] + W_CLASS - 1) / W_CLASS * W_CLASS;
-  }
-  // the rows, in order within each class
-  for (int base = 0; base < n; base += CHUNK) {
-    if (n > CHUNK) {  // (else they are still held)
-      classify(base);
-      scan();
-    }
+    const int total = before[k][64];
 #pragma unroll
     for (int u = 0; u < PLAN_U; ++u)
-#pragma unroll
-      for (int k = 0; k < 3; ++k)
-        if (c[u] == k) {
-          const int row = base + u * PLAN_THREADS + tid;
-          const bool cl = k == 2 && v[u] == j[u] && j[u] >= tok0 && j[u] <= last;
-          const int64_t e = at + done[k] + before[k][u * PLAN_WAVES + wave] + mask_rank(m[k][u]);
-          p.row[e] = cl ? row | W_CL : row;
-          p.tok[e] = j[u];
-          p.vu[e] = k == 2 ? -1 : v[u];
-        }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) done[k] += before[k][64];
-  }
-  // what fills a class's last tiles: row -1, seen by none
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    const int end = k < 2 ? first[k + 1] : start;
-    for (int e = first[k] + total[k] + tid; e < end; e += PLAN_THREADS) {
+      if (c[u] == k) {
+        const int row = row0 + u * PLAN_THREADS + tid;
+        const bool cl = k == 2 && v[u] == j[u] && j[u] >= tok0 && j[u] <= last;
+        const int64_t e = at + start + before[k][u * PLAN_WAVES + wave] + mask_rank(m[k][u]);
+        p.row[e] = cl ? row | W_CL : row;
+        p.tok[e] = j[u];
+        p.vu[e] = k == 2 ? -1 : v[u];
+      }
+    const int next = k == 2 ? p.chunk : start + (total + W_CLASS - 1) / W_CLASS * W_CLASS;
+    for (int e = start + total + tid; e < next; e += PLAN_THREADS) {
       p.row[at + e] = -1;
       p.tok[at + e] = 0x7fffffff;
       p.vu[at + e] = -1;
     }
+    start = next;
   }
   __threadfence_block();
   __syncthreads();
-  const int tiles = start / W_TILE;
-  for (int t = tid / 32; t < tiles; t += PLAN_THREADS / 32) {
-    const int j = p.tok[at + t * W_TILE + (tid & 31)], v = p.vu[at + t * W_TILE + (tid & 31)];
-    TileSum x = {j, j, v, v};
+  for (int t = tid / 32; t < p.chunk / W_TILE; t += PLAN_THREADS / 32) {
+    const int jt = p.tok[at + t * W_TILE + (tid & 31)], vt = p.vu[at + t * W_TILE + (tid & 31)];
+    TileSum x = {jt, jt, vt, vt};
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
       x.tmin = min(x.tmin, __shfl_xor(x.tmin, off, 64));
@@ -184,9 +166,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void weight_plan_kernel(
       x.vmin = min(x.vmin, __shfl_xor(x.vmin, off, 64));
       x.vmax = max(x.vmax, __shfl_xor(x.vmax, off, 64));
     }
-    if ((tid & 31) == 0) p.sum[(int64_t)s * (p.entries / W_TILE) + t] = x;
+    if ((tid & 31) == 0) p.sum[at / W_TILE + t] = x;
   }
-  if (tid == 0) p.tiles[s] = make_int2(first[2] / W_TILE, tiles);
 }
 
 // ---------------------------------------------------------------------------
@@ -299,7 +280,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_stats_kernel(
   const int64_t at = (int64_t)s * p.entries;
   const int32_t *rows = p.row + at, *toks = p.tok + at, *vus = p.vu + at;
   const TileSum* sums = p.sum + (int64_t)s * (p.entries / W_TILE);
-  const int n_tiles = p.tiles[s].x;
+  const int n_tiles = p.tiles[s];
 
   Operand<T, D> Q[QT];
   int t[QT], ta[QT], tb[QT];  // the lane's token; first and last of the tile's
@@ -395,31 +376,33 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_stats_kernel(
   }
 }
 
-// the normaliser of query i, from the shares' maxima and sums (+inf: the query
-// gives nothing); the halves of the wave take every other share
+// (maximum, sum) of two sets of rows, and the normaliser of one (+inf: the query
+// gives nothing)
+__device__ __forceinline__ float2 join_norm(float2 a, float2 b) {
+  const float m = fmaxf(a.x, b.x);
+  if (m == -INFINITY) return make_float2(m, 0.f);
+  return make_float2(m, a.y * fast_exp2(a.x - m) + b.y * fast_exp2(b.x - m));
+}
+__device__ __forceinline__ float norm_lse(float2 a) {
+  return a.y > 0.f ? a.x + __builtin_amdgcn_logf(a.y) : INFINITY;
+}
+// query i over the shares first, first + step, ..., the wave's halves together
+__device__ __forceinline__ float2 tile_norm(const float2* __restrict__ ml, int i, int nq, int first,
+                                            int step, int splits) {
+  float2 a = make_float2(-INFINITY, 0.f);
+  if (i < nq) {
+#pragma unroll 4
+    for (int j = first; j < splits; j += step) a = join_norm(a, ml[(int64_t)j * nq + i]);
+  }
+  const auto m = __builtin_amdgcn_permlane32_swap(__float_as_uint(a.x), __float_as_uint(a.x), false, false);
+  const auto l = __builtin_amdgcn_permlane32_swap(__float_as_uint(a.y), __float_as_uint(a.y), false, false);
+  return join_norm(make_float2(__uint_as_float(m[0]), __uint_as_float(l[0])),
+                   make_float2(__uint_as_float(m[1]), __uint_as_float(l[1])));
+}
 __device__ __forceinline__ float tile_lse(const float2* __restrict__ ml, int i, int nq, int splits,
                                           int h) {
-  float m = -INFINITY, l = 0.f;
-  if (i < nq) {
-    if (splits == 1) {
-      const float2 x = ml[i];
-      m = x.x;
-      l = x.y;
-    } else {
-      for (int j = h; j < splits; j += 2) {
-        const float2 x = ml[(int64_t)j * nq + i];
-        const float mn = fmaxf(m, x.x);
-        if (mn != -INFINITY) l = l * fast_exp2(m - mn) + x.y * fast_exp2(x.x - mn);
-        m = mn;
-      }
-    }
-  }
-  if (splits > 1) {
-    const float mn = other_half(m, false);
-    l = other_half(m == -INFINITY ? 0.f : l * fast_exp2(m - mn), true);
-    m = mn;
-  }
-  return l > 0.f ? m + __builtin_amdgcn_logf(l) : INFINITY;
+  if (splits == 1) return i < nq ? norm_lse(ml[i]) : INFINITY;
+  return norm_lse(tile_norm(ml, i, nq, h, 2, splits));
 }
 
 // ---------------------------------------------------------------------------
@@ -436,7 +419,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wg = blockIdx.x / n_slice, slice = blockIdx.x - wg * n_slice;
   const int s = slice / H;
-  const int n_tiles = p.tiles[s].y;  // a multiple of two
+  const int n_tiles = p.tiles[s];  // a multiple of two
   const int t0 = (wg * (W_WAVES / WQ) + (WQ == 1 ? wave : 0)) * KT;
   if (t0 >= n_tiles) return;  // (all waves of a workgroup alike where WQ > 1)
   const T* qb = q + slice * q_s;
@@ -599,7 +582,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_stats_staged_kernel(
   const T* kb = k + slice * k_s;
   const int64_t at = (int64_t)s * p.entries;
   const TileSum* sums = p.sum + (int64_t)s * (p.entries / W_TILE);
-  const int n_stage = p.tiles[s].x / 2;
+  const int n_stage = p.tiles[s] / 2;
   const int q0 = g0 + wave * QT * W_TILE;
 
   Operand<T, D> Q[QT];
@@ -716,7 +699,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wg = blockIdx.x / n_slice, slice = blockIdx.x - wg * n_slice;
   const int s = slice / H;
-  const int n_tiles = p.tiles[s].y;
+  const int n_tiles = p.tiles[s];
   const int g0 = wg * W_WAVES * KT;  // first tile of the workgroup
   if (g0 >= n_tiles) return;
   const T* qb = q + slice * q_s;
@@ -819,7 +802,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
 // sums of few queries (QT tiles): a wave keeps all queries and streams `run`
 // key tiles, the next tile's keys and sums in flight while one is computed.
 // With the keys kept instead, a wave's chain of loads (row numbers, keys, old
-// sums) was paid every 64 rows: 49 us against VOTES_US for 32 queries over
+// sums) was paid every 64 rows: 49 us against 28 for 32 queries over
 // 512 slices of 2050 rows of 80.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int QT>
@@ -831,13 +814,30 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
   const int wg = blockIdx.x / n_slice, slice = blockIdx.x - wg * n_slice;
   const int unit = __builtin_amdgcn_readfirstlane(wg * W_WAVES + (threadIdx.x >> 6));
   const int s = slice / H;
-  const int n_tiles = p.tiles[s].y;
+  const int n_tiles = p.tiles[s];
   const int t0 = unit * run, t1 = min(t0 + run, n_tiles);
+  // the normalisers: each wave joins a quarter of the shares
+  __shared__ float2 meet[W_WAVES][QT * W_TILE];
+  const int wave = threadIdx.x >> 6;
+  const float2* mls = ml + (int64_t)slice * splits * nq;
+  float lse[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const float2 part = tile_norm(mls, W_TILE * x + l32, nq, wave * 2 + h, 2 * W_WAVES, splits);
+    if (lane < 32) meet[wave][W_TILE * x + l32] = part;
+  }
+  __syncthreads();
   if (t0 >= t1) return;
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    float2 all = meet[0][W_TILE * x + l32];
+#pragma unroll
+    for (int w = 1; w < W_WAVES; ++w) all = join_norm(all, meet[w][W_TILE * x + l32]);
+    lse[x] = norm_lse(all);
+  }
   const T* kb = k + slice * k_s;
   const int64_t at = (int64_t)s * p.entries;
   const TileSum* sums = p.sum + (int64_t)s * (p.entries / W_TILE);
-  const float2* mls = ml + (int64_t)slice * splits * nq;
   const int last = tok0 + nq - 1;
   // the row of a tile whose sum this lane ends with
   int base = 0;
@@ -857,12 +857,8 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
   load(A, number(t0, l32));
   float o0 = old(e0);
   Operand<T, D> Q[QT];
-  float lse[QT];
 #pragma unroll
-  for (int x = 0; x < QT; ++x) {
-    Q[x].load(q + slice * q_s + (int64_t)min(W_TILE * x + l32, nq - 1) * D, h);
-    lse[x] = tile_lse(mls, W_TILE * x + l32, nq, splits, h);
-  }
+  for (int x = 0; x < QT; ++x) Q[x].load(q + slice * q_s + (int64_t)min(W_TILE * x + l32, nq - 1) * D, h);
   auto compute = [&](const Operand<T, D>& K, int t, int e, float before) {
     const TileSum ts = sums[t];
     float v[16];
@@ -963,7 +959,10 @@ static int launch_weights(const void* q, const void* k, const float* w_in, float
   const int slices = b * H;
   const float c = scale * W_LOG2E;
   const WeightShape sh = weight_shape(BF16, slices, nq, L_cap);
-  weight_plan_kernel<<<b, PLAN_THREADS, 0, stream>>>(p, vu, L_meta, tok0, nq, kv_len, tok_idx, L_cap);
+  const int chunks = plan_chunks(L_cap);
+  if ((int64_t)b * chunks > 0x7fffffff) return fail(SCKV_EUNSUP, "cached_attn_weights: too many tiles");
+  weight_plan_kernel<<<b * chunks, PLAN_THREADS, 0, stream>>>(p, vu, L_meta, tok0, nq, kv_len, tok_idx,
+                                                             L_cap, chunks);
   int rc = hip_check(hipGetLastError(), "cached_attn_weights: plan launch");
   if (rc) return rc;
   unsigned g = 0;  // workgroups
