@@ -535,7 +535,8 @@ int compacted_decode_attn_weights(const void* q, const void* k_new, const void* 
  * w, w_out : (M, b, H, L_cap) float sums, moved as the rows are (w_out
  *            nullable: in place); those behind the survivors become 0.
  * heavy, recent : >= 0, heavy + recent >= 1.
- * kv_len, tok_idx, pos_ids : in/out, as for kv_compact.
+ * kv_len, tok_idx, pos_ids : in/out, as for kv_compact (kv_len clamped to
+ *            [0, L_cap]).
  * total    : [b][L_cap] float out: the totals of rows [0, kv_len[s]) as they
  *            were before the call; rows behind are left as they are.
  * kept_src_row : [b][L_cap] out, as for kv_compact.

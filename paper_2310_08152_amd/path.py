@@ -239,6 +239,8 @@ def norm_rope_rows(q, k, v, qr, k_out, v_out, norm: QKNorm, meta: SpanMeta, n: i
     any strides, for instance of a projection's token-major output; those of
     one stride pattern share a launch."""
     b, H, _, d = q.shape
+    if not q.shape[2] == k.shape[2] == v.shape[2] == n:
+        q, k, v = (t[:, :, :n] for t in (q, k, v))
     x = q.stride()
     sets = ([(q, k, v, qr, k_out, v_out)] if k.stride() == x and v.stride() == x else
             [(q, None, None, qr, None, None), (None, k, None, None, k_out, None),
@@ -281,6 +283,12 @@ def decode_layer(q, k_new, v_new, cache: KVCache, m: int, meta: SpanMeta, ws: Wo
                             cache.status, stream=stream)
 
 
+def _sums_of(cache: KVCache, m: int):
+    if cache.w is None:
+        raise ValueError("no accumulated weights: call the cache's track_weights, or pass w_out")
+    return cache._w[m]
+
+
 def decode_weights_layer(q, k_new, v_new, cache: KVCache, m: int, meta: SpanMeta, ws: Workspace,
                          o, w_in=None, w_out=None, scale=None, theta: float = 0.0, stream=None,
                          norm: QKNorm = None):
@@ -289,7 +297,7 @@ def decode_weights_layer(q, k_new, v_new, cache: KVCache, m: int, meta: SpanMeta
     sums (track_weights)."""
     d = q.shape[-1]
     if w_out is None:
-        w_in = w_out = cache._w[m]
+        w_in = w_out = _sums_of(cache, m)
     q, k_new, theta = _normed(norm, q, k_new, cache, meta, theta, stream)
     B.compacted_decode_attn_weights(q, k_new, v_new, cache.k(m), cache.v(m), cache.kv_len,
                                     cache.cur_tok, meta.vu, meta.pos, meta.L_meta, o, w_in, w_out,
@@ -306,7 +314,7 @@ def prompt_weights(q, cache: KVCache, m: int, meta: SpanMeta, ws: Workspace, tok
     are; its last queries alone make a vote of recent tokens."""
     b, H, nq, d = q.shape
     if w_out is None:
-        w_in = w_out = cache._w[m]
+        w_in = w_out = _sums_of(cache, m)
     B.cached_attn_weights(q, cache.k(m), w_in, w_out, b, H, nq, d, q.stride(1),
                           cache.k(m).stride(1), default_scale(d) if scale is None else scale,
                           meta.vu, meta.L_meta, tok0, cache.kv_len, cache.tok_idx, cache.L_cap,
@@ -367,9 +375,11 @@ def prefill_progressive(q, k, v, o, cache: KVCache, meta: SpanMeta, ws: Workspac
     beyond that budget leave after the block, so the cache needs room for
     heavy + recent + block rows and later blocks attend over what is left."""
     M, b, H, _, d = q.shape
-    cache.kv_len.zero_()
     if evict is not None:
+        if cache.w is None or ws.weights is None:
+            raise ValueError("evict needs cache.track_weights() and a workspace with weights=block")
         cache.w.zero_()
+    cache.kv_len.zero_()
     row0 = torch.empty(b, dtype=torch.int32, device=q.device)
     nxt = torch.empty(b, dtype=torch.int32, device=q.device)
     qr = torch.empty(b, H, block, d, dtype=q.dtype, device=q.device)

@@ -177,8 +177,18 @@ def test_path_refuses(B):
         c.evict(1, 1)
     with pytest.raises(ValueError):
         c.track_weights(torch.zeros(1, 1, 2, 9))
+    meta, x = None, torch.zeros(1, 2, 1, 64)
+    with pytest.raises(ValueError):
+        P.prompt_weights(x, c, 0, meta, None, 0)
+    with pytest.raises(ValueError):
+        P.decode_weights_layer(x[:, :, 0], x[:, :, 0], x[:, :, 0], c, 0, meta, None, x)
     c.track_weights()
     assert c.w.shape == (1, 1, 2, 8)
+    c.kv_len.fill_(3)
+    with pytest.raises(ValueError):  # no workspace for weights: refused before anything changes
+        P.prefill_progressive(x[None], x[None], x[None], x[None], c, meta,
+                              type("Ws", (), {"weights": None}), 1, 1, evict=(1, 1))
+    assert int(c.kv_len[0]) == 3
 
 
 @pytest.mark.parametrize("source", ("norm_rope", "evict", "weights", "shared"))

@@ -95,6 +95,31 @@ def test_prompt(b, H, n, d, dtype, layout, theta):
     assert bool((kv[:, :, :, n:] == 7.0).all())
 
 
+@pytest.mark.parametrize("b,H,n,d,dtype,layout", [
+    (2, 33, 500, 80, "bf16", "tokens"),      # four heads a thread, a tensor a workgroup
+    (3, 6, 800, 64, "f32", "fused-heads"),
+    (2, 33, 8000, 64, "bf16", "tokens"),     # four heads of q, k and v a thread
+    (1, 35, 5700, 80, "f32", "tokens"),      # two
+])
+def test_large_launches(b, H, n, d, dtype, layout):
+    print("norm large", b, H, n, d, dtype, layout, flush=True)
+    dt, spans = DT[dtype], [R.some_spans(n, 3)] * b
+    meta = P().SpanMeta(spans, n, DEV)
+    pos = R.vu_pos(spans[0], n)[1]
+    q, k, v = to_dev(views(b, H, n, d, dt, layout, 5))
+    nm = P().QKNorm(*[w.to(DEV) for w in weights(d, dt, 4)], EPS)
+    qr = torch.empty(b, H, n, d, dtype=dt, device=DEV)
+    kv = torch.empty(2, b, H, n, d, dtype=dt, device=DEV)
+    P().norm_rope_rows(q, k, v, qr, kv[0], kv[1], nm, meta, n, 0, 1e4)
+    assert torch.equal(kv[1], v)
+    for x, w, got in ((q, nm.q_weight, qr), (k, nm.k_weight, kv[0])):
+        for s in range(b):
+            want = R.norm_rope(x[s], w, EPS, pos, 1e4)
+            tol = R.norm_rope_tol(x[s], w, EPS, dt)
+            tol = tol + R.half_step(dt) * (want.abs() + tol)
+            assert not ((got[s].double() - want).abs() > tol).any(), s
+
+
 def test_forms_of_one_operand_and_without_weights():
     b, H, n, d, dt = 2, 3, 21, 80, torch.bfloat16
     print("norm single operands", flush=True)

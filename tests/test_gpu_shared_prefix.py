@@ -151,6 +151,29 @@ def test_large_scores_and_unwritten_rows():
             x.check(s, 1e4)
 
 
+def test_prefix_offsets_beyond_32_bits():
+    """A prefix cache of more than 2^31 elements: the last heads."""
+    print("shared far offsets", flush=True)
+    H, P_cap, d, m, per = 33, 1 << 20, 64, 300, 3
+    kv = torch.empty(2, 2, 1, H, P_cap, d, dtype=torch.bfloat16, device=DEV)[1:]
+    pre = P().KVCache(1, 1, H, P_cap, d, torch.bfloat16, DEV, kv=kv)
+    kv[:, :, :, :, :m] = R.rand((1, 2, 1, H, m, d), 3, torch.bfloat16, device=DEV)
+    kv[:, :, :, :, m:m + 8] = float("nan")
+    pre.kv_len.fill_(m)
+    meta = P().SpanMeta([[]] * per, m + 8, DEV)
+    c = P().KVCache(1, per, H, 4, d, torch.bfloat16, DEV)
+    c.start_behind(m)
+    ws = P().Workspace(per, H, 1, 4, d, DEV, prefixes=1, prefix_rows=P_cap)
+    qkv = [R.rand((per, H, d), i, torch.bfloat16, device=DEV) for i in range(3)]
+    o = torch.empty(per, H, d, dtype=torch.bfloat16, device=DEV)
+    P().shared_decode_layer(*qkv, pre, c, 0, meta, ws, o)
+    for s in range(per):
+        k, v = (torch.cat([kv[0, i, 0, :, :m].cpu(), qkv[1 + i][s].cpu()[:, None]], 1)
+                for i in range(2))
+        want = R.attend(qkv[0][s].cpu(), k, v, d ** -0.5)[0]
+        assert float((o[s].cpu().double() - want).abs().max()) < 2e-2
+
+
 def test_equals_one_cache_holding_both():
     """The same rows in one cache: decode_layer gives the same step (to the
     rounding of the two)."""

@@ -177,6 +177,35 @@ def test_strided_queries_other_scale_and_sharp_ties():
     h.check(out, torch.zeros_like(out), L - nq)
 
 
+@pytest.mark.parametrize("nq,H,L", [(5, 2, 300), (90, 3, 300), (64, 90, 700)])
+def test_prompt_weights_graph_and_stream(nq, H, L):
+    """A side stream and replays of a graph give the eager bits; another call on
+    the same workspace runs between the replays."""
+    print("weights graph", nq, H, L, flush=True)
+    b, d = 2, 64
+    spans = [R.some_spans(L, s) for s in range(b)]
+    h = Held(b, H, L, d, torch.bfloat16, L, spans, [list(range(L))] * b, 8, nq)
+    w_in = R.rand((b, H, L), 3, torch.float32, device=DEV)
+    outs = [torch.zeros_like(w_in) for _ in range(3)]
+    call = lambda o, q=h.q: P().prompt_weights(q, h.cache, 0, h.meta, h.ws, L - nq, w_in, o)
+    call(outs[0])
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        call(outs[1])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(outs[2])
+    for _ in range(3):
+        outs[2].zero_()
+        call(outs[1], -h.q)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[2])
+
+
 # ---------------------------------------------------------------------------
 # decode steps
 # ---------------------------------------------------------------------------
@@ -235,6 +264,8 @@ DECODE = [
     (2, 2, 64, "f32", 2500, [2499, 1200], 1e4),    # fp32, split
     (20, 32, 80, "f32", 130, None, 0.0),           # fp32, one workgroup a slice
     (40, 32, 64, "f32", 50, None, 1e4),            # fp32, narrow
+    (1, 520, 64, "bf16", 16384, [16000], 1e4),     # the most scores kept in LDS
+    (1, 520, 64, "bf16", 16500, [16400], 0.0),     # one workgroup a slice, scores in memory
 ]
 
 
@@ -295,6 +326,32 @@ def test_decode_weights_special_steps(cap, b, H, dtype):
                  2.0 ** -17 if dtype == "bf16" else 0.0)
     P().decode_weights_layer(*qkv, cache, 1, meta, ws, o, None, out, theta=1e4)
     assert bool((out[0, :, :20] == 0).all())
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of more than 2^31 elements: the last slices' rows and sums."""
+    print("decode weights far offsets", flush=True)
+    b, H, cap, d, n = 1, 33, 1 << 20, 64, 150
+    meta = P().SpanMeta([[]], 200, DEV)
+    kv = torch.empty(1, 2, b, H, cap, d, dtype=torch.bfloat16, device=DEV)
+    cache = P().KVCache(1, b, H, cap, d, torch.bfloat16, DEV, kv=kv)
+    kv[:, :, :, :, :n + 2] = R.rand((1, 2, b, H, n + 2, d), 3, torch.bfloat16, device=DEV)
+    before = kv[0, :, :, :, :n + 2].cpu()
+    cache.kv_len.fill_(n)
+    cache.cur_tok.fill_(n)
+    w_in = torch.ones(b, H, cap, device=DEV)
+    out = torch.empty(b, H, cap, device=DEV)
+    ws = P().Workspace(b, H, 1, cap, d, DEV, weights=1)
+    qkv = [R.rand((b, H, d), i, torch.bfloat16, device=DEV) for i in range(3)]
+    o = torch.empty(b, H, d, dtype=torch.bfloat16, device=DEV)
+    P().decode_weights_layer(*qkv, cache, 0, meta, ws, o, w_in, out)
+    k, v = before[0, 0, :, :n + 1].clone(), before[1, 0, :, :n + 1].clone()
+    k[:, n], v[:, n] = qkv[1][0].cpu(), qkv[2][0].cpu()
+    want, p, _, _ = R.attend(qkv[0][0].cpu(), k, v, d ** -0.5)
+    assert float((o[0].cpu().double() - want).abs().max()) < 2e-2
+    p[:, :n] += 1
+    assert float((out[0, :, :n + 1].cpu().double() - p).abs().max()) < 1e-5
+    assert torch.equal(kv[0, :, 0, :, n + 1].cpu(), before[:, 0, :, n + 1])
 
 
 @pytest.mark.parametrize("b,H,cap", [(2, 3, 1500), (3, 200, 100)])
