@@ -291,7 +291,14 @@ def test_decode_weights(b, H, d, dtype, cap, lens, theta):
                      2.0 ** -17 if dtype == "bf16" else 0.0)
     for s in range(b):
         assert bool((out[s, :, lens[s] + 1:] == -3.0).all())
-    assert torch.equal(cache.kv.cpu(), ref.kv.cpu())  # the appended row included
+    # the other rows are left alone, and the new ones are decode_layer's to one
+    # rounding (its rotation is in 32 bits)
+    other = ref.kv.clone()
+    for s in range(b):
+        a, c = (x[1, 0, s, :, lens[s]].double() for x in (cache.kv, ref.kv))
+        assert bool(((a - c).abs() <= 2.5 * R.half_step(dt) * c.abs() + 64 * R.U).all())
+        other[1, 0, s, :, lens[s]] = cache.kv[1, 0, s, :, lens[s]]
+    assert torch.equal(cache.kv, other)
     assert int(cache.status[0]) == 0
     assert torch.equal(cache.w[1].cpu(), w_before)
     # in place on the cache's sums
