@@ -903,7 +903,8 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
 //    32 heads of 2048 tokens: 74, 67), else one.  The rows are cut into
 //    up to 64 shares of at least 128 until there are W_FILL waves, two a SIMD.
 //  * sums: up to 32 queries (bf16: 64) are kept by every wave, which streams
-//    rows (`votes`: as many waves as stay resident, up to 16 tiles each).
+//    rows (`votes`: W_FILL waves, up to 16 tiles each; 16 x 64 queries over 2048
+//    rows of 80: 66, with 4096 waves 69; 32 heads of 16000 rows 38, 41).
 //    Beyond, a wave keeps two tiles of bf16 rows where W_FILL waves do, else
 //    one, and the waves of a workgroup share theirs below W_SHARE tiles (32
 //    heads of 2048 tokens: 93 a wave each, 74 shared).
@@ -912,7 +913,6 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
 constexpr int W_FILL = 2048;
 constexpr int W_UNITS = 512;
 constexpr int W_SHARE = 4096;
-constexpr int W_RESIDENT = 3072;
 constexpr int W_LONG = 4096;
 constexpr int W_WGS = 512;
 
@@ -991,7 +991,7 @@ static int launch_weights(const void* q, const void* k, const float* w_in, float
                                       slices, sh.splits);
   };
   if (sh.votes > 0) {
-    const int run = (int)std::min<int64_t>(16, std::max<int64_t>(1, slices * tiles / W_RESIDENT));
+    const int run = (int)std::min<int64_t>(16, std::max<int64_t>(1, slices * tiles / W_FILL));
     const int64_t units = (tiles + run - 1) / run;
     rc = grid((units + W_WAVES - 1) / W_WAVES);
     if (rc) return rc;
