@@ -520,7 +520,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_kernel(
 // Stages: 64 rows (two tiles) that a workgroup's waves share through LDS,
 // for long lists: a wave's own loads of an operand touch 32 cache lines an
 // instruction, 32 bytes of each; staged, a line is read once a workgroup
-// (16384 queries, 32 heads of 64: 1180 -> 923 us).  Short lists are slower so
+// (16384 queries, 32 heads of 64: 1180 -> 970 us).  Short lists are slower so
 // (16 x 1024 queries of 80: 152 -> 207 us): a workgroup's four waves go through
 // the union of their lists, a barrier a stage.
 // Piece g of row r lies at g ^ (r % 8) where a row is a power of two of
@@ -564,9 +564,14 @@ struct Stage {
   }
 };
 
+// Waves of a SIMD that the registers are held to: four where one register less
+// gives them (d = 64; 2 x 32 heads of 4096 tokens 222 -> 190 us), else what the
+// compiler leaves.
+constexpr int staged_waves(bool bf16, int D, bool fits) { return bf16 && D == 64 && fits ? 4 : 2; }
+
 // stats of large launches: QT tiles of queries a wave, W_WAVES * QT a workgroup
 template <typename T, int D, int QT>
-__global__ __launch_bounds__(64 * W_WAVES, 2) void weight_stats_staged_kernel(
+__global__ __launch_bounds__(64 * W_WAVES, staged_waves(sizeof(T) == 2, D, true)) void weight_stats_staged_kernel(
     const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, float2* __restrict__ ml,
     int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c, const int32_t* __restrict__ vu,
     int32_t L_meta, int32_t tok0, int32_t n_slice, int32_t qgroups, int32_t splits) {
@@ -688,7 +693,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_stats_staged_kernel(
 
 // sums of large launches: KT tiles of rows a wave, W_WAVES * KT a workgroup
 template <typename T, int D, int KT>
-__global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
+__global__ __launch_bounds__(64 * W_WAVES, staged_waves(sizeof(T) == 2, D, KT == 1)) void weight_sums_staged_kernel(
     const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, const float2* __restrict__ ml,
     const float* w_in, float* w_out, int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c,
     int32_t tok0, int32_t L_cap, int32_t n_slice, int32_t splits) {
@@ -909,7 +914,12 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
 //    one, and the waves of a workgroup share theirs below W_SHARE tiles (32
 //    heads of 2048 tokens: 93 a wave each, 74 shared).
 //  * from W_LONG rows and W_LONG / 4 queries on, with W_WGS workgroups: both
-//    staged in LDS.
+//    staged in LDS.  A wave keeps two tiles of queries where 2 W_WGS workgroups
+//    do (32 heads of 8192 tokens of 80: 558 with two, 587 with one), else one
+//    (4096 tokens: 198, 179).  Two tiles of rows where 4 W_WGS workgroups do (32
+//    heads of 16384 tokens of 64: 1000, 1050 with one; 2 x 32 heads of 4096:
+//    213, 190), but of 64 elements only: of 80 their registers leave two waves
+//    a SIMD (16 x 4096 tokens: 1872, 1593).
 constexpr int W_FILL = 2048;
 constexpr int W_UNITS = 512;
 constexpr int W_SHARE = 4096;
@@ -932,8 +942,8 @@ static WeightShape weight_shape(bool bf16, int64_t slices, int32_t nq, int32_t L
   const int64_t groups = (nq + group - 1) / group;
   w.staged = nq >= W_LONG / 4 && L_cap >= W_LONG && slices * groups >= W_WGS;
   if (w.staged) {
-    w.keep = two;
-    w.qtiles = (int)groups;
+    if (slices * groups >= 2 * W_WGS) w.keep = two;
+    w.qtiles = (nq + W_WAVES * W_TILE * w.keep - 1) / (W_WAVES * W_TILE * w.keep);
     return w;
   }
   const int pair = two * W_TILE;
@@ -979,7 +989,8 @@ static int launch_weights(const void* q, const void* k, const float* w_in, float
       kernel<<<g, THREADS, 0, stream>>>(qq, kk, p, ml, H, nq, q_s, k_s, c, vu, L_meta, tok0, slices,
                                         sh.qtiles, sh.splits);
     };
-    if (sh.staged) go(weight_stats_staged_kernel<T, D, NT>);
+    if (sh.staged && sh.keep == NT) go(weight_stats_staged_kernel<T, D, NT>);
+    else if (sh.staged) go(weight_stats_staged_kernel<T, D, 1>);
     else if (sh.keep == NT) go(weight_stats_kernel<T, D, NT>);
     else go(weight_stats_kernel<T, D, 1>);
     rc = hip_check(hipGetLastError(), "cached_attn_weights: stats launch");
@@ -1002,9 +1013,12 @@ static int launch_weights(const void* q, const void* k, const float* w_in, float
     if (sh.votes == NT) vote(weight_votes_kernel<T, D, NT>);
     else vote(weight_votes_kernel<T, D, 1>);
   } else if (sh.staged) {
-    rc = grid((tiles + W_WAVES * NT - 1) / (W_WAVES * NT));
+    constexpr int KT = D == 64 ? NT : 1;
+    const int kt = slices * (tiles / (W_WAVES * KT)) >= 4 * W_WGS ? KT : 1;
+    rc = grid((tiles + W_WAVES * kt - 1) / (W_WAVES * kt));
     if (rc) return rc;
-    go(weight_sums_staged_kernel<T, D, NT>);
+    if (kt == KT) go(weight_sums_staged_kernel<T, D, KT>);
+    else go(weight_sums_staged_kernel<T, D, 1>);
   } else {
     const int kt = slices * (tiles / NT) >= W_FILL ? NT : 1;
     const int wq = kt == 1 && slices * tiles < W_SHARE ? W_WAVES : 1;

@@ -79,6 +79,10 @@ CASES = [
     (4, 64, 80, "bf16", 300, 131, True, 0.4),
     (1, 64, 64, "bf16", 4100, 2100, False, 0.6),  # staged
     (1, 110, 80, "f32", 4100, 1030, True, 0.2),
+    (1, 64, 64, "bf16", 4091, 2100, False, 0.4),  # ... one tile of rows a wave
+    (1, 205, 64, "bf16", 4100, 1025, True, 0.4),  # ... two of queries
+    (1, 205, 80, "bf16", 4100, 1025, False, 0.5),
+    (1, 110, 80, "bf16", 4100, 1250, False, 0.3),
     (40, 13, 64, "bf16", 520, 5, False, 0.3),     # two tiles of rows, one of queries
     (3, 100, 80, "f32", 260, 45, False, 0.5),
 ]
