@@ -26,6 +26,7 @@
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "sckv_common.h"
 
@@ -55,6 +56,7 @@ constexpr int PLAN_WAVES = 16;
 constexpr int PLAN_THREADS = 64 * PLAN_WAVES;
 constexpr int PLAN_U = 4;  // rows of a thread, in flight together
 constexpr int PLAN_CHUNK = PLAN_THREADS * PLAN_U;
+constexpr int PLAN_ENTRIES = PLAN_CHUNK + 3 * W_CLASS;  // the most of a chunk's list
 
 // Entries of a sequence's list.  Each PLAN_CHUNK rows have a part of their own
 // (a workgroup plans it): every row, and each class up to W_CLASS - 1 more.
@@ -80,6 +82,20 @@ static WeightPlan plan_at(void* ws, int32_t b, int32_t L_cap) {
   return p;
 }
 
+// `of` over the 32 lanes of each half-wave; every lane gets it
+template <typename F>
+__device__ __forceinline__ int half_wave_of(int x, F of) {
+  const auto mov = [](int y, auto ctrl) {
+    return __builtin_bit_cast(int, dpp_mov<decltype(ctrl)::value>(__builtin_bit_cast(float, y)));
+  };
+  x = of(x, mov(x, std::integral_constant<int, DPP_QUAD_XOR1>()));
+  x = of(x, mov(x, std::integral_constant<int, DPP_QUAD_XOR2>()));
+  x = of(x, mov(x, std::integral_constant<int, DPP_ROW_HALF_MIRROR>()));
+  x = of(x, mov(x, std::integral_constant<int, DPP_ROW_MIRROR>()));
+  const auto r = __builtin_amdgcn_permlane16_swap((unsigned)x, (unsigned)x, false, false);
+  return of((int)r[0], (int)r[1]);
+}
+
 // one workgroup per chunk of a sequence
 __global__ __launch_bounds__(PLAN_THREADS) void weight_plan_kernel(
     WeightPlan p, const int32_t* __restrict__ vu, int32_t L_meta, int32_t tok0, int32_t nq,
@@ -89,23 +105,26 @@ __global__ __launch_bounds__(PLAN_THREADS) void weight_plan_kernel(
   // rows of class k that pass u of wave w holds, then those before them, at
   // [k][u * PLAN_WAVES + w]; the total behind them
   __shared__ int before[3][65];
+  // tokens and vu of the chunk's list, for the summaries of its tiles
+  __shared__ int list_tok[PLAN_ENTRIES], list_vu[PLAN_ENTRIES];
   const int s = blockIdx.x / chunks, chunk = blockIdx.x - s * chunks;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row0 = chunk * PLAN_CHUNK;
+  const int32_t* toks = tok_idx + (int64_t)s * L_cap + row0;
+  const int32_t* vus = vu + (int64_t)s * L_meta;
+  // (asked for before the length is known: rows past it are read and dropped)
+  int j[PLAN_U], v[PLAN_U], c[PLAN_U];
+#pragma unroll
+  for (int u = 0; u < PLAN_U; ++u) j[u] = toks[min(u * PLAN_THREADS + tid, L_cap - 1 - row0)];
   const int held = min(max(kv_len[s], 0), L_cap);
   if (chunk == 0 && tid == 0)
     p.tiles[s] = (held + PLAN_CHUNK - 1) / PLAN_CHUNK * (p.chunk / W_TILE);
-  const int row0 = chunk * PLAN_CHUNK;
   const int n = min(held - row0, PLAN_CHUNK);  // rows of this chunk
   if (n <= 0) return;
-  const int32_t* toks = tok_idx + (int64_t)s * L_cap + row0;
-  const int32_t* vus = vu + (int64_t)s * L_meta;
   const int64_t at = (int64_t)s * p.entries + (int64_t)chunk * p.chunk;
   const int last = tok0 + nq - 1;  // last query's token
   // classes: 0 seen by every later query, 1 by some, 2 by none (3: no row)
-  int j[PLAN_U], v[PLAN_U], c[PLAN_U];
   uint64_t m[3][PLAN_U];
-#pragma unroll
-  for (int u = 0; u < PLAN_U; ++u) j[u] = toks[min(u * PLAN_THREADS + tid, n - 1)];
 #pragma unroll
   for (int u = 0; u < PLAN_U; ++u) v[u] = vus[min(max(j[u], 0), L_meta - 1)];
 #pragma unroll
@@ -141,31 +160,26 @@ __global__ __launch_bounds__(PLAN_THREADS) void weight_plan_kernel(
       if (c[u] == k) {
         const int row = row0 + u * PLAN_THREADS + tid;
         const bool cl = k == 2 && v[u] == j[u] && j[u] >= tok0 && j[u] <= last;
-        const int64_t e = at + start + before[k][u * PLAN_WAVES + wave] + mask_rank(m[k][u]);
-        p.row[e] = cl ? row | W_CL : row;
-        p.tok[e] = j[u];
-        p.vu[e] = k == 2 ? -1 : v[u];
+        const int e = start + before[k][u * PLAN_WAVES + wave] + mask_rank(m[k][u]);
+        p.row[at + e] = cl ? row | W_CL : row;
+        p.tok[at + e] = list_tok[e] = j[u];
+        p.vu[at + e] = list_vu[e] = k == 2 ? -1 : v[u];
       }
     const int next = k == 2 ? p.chunk : start + (total + W_CLASS - 1) / W_CLASS * W_CLASS;
     for (int e = start + total + tid; e < next; e += PLAN_THREADS) {
       p.row[at + e] = -1;
-      p.tok[at + e] = 0x7fffffff;
-      p.vu[at + e] = -1;
+      p.tok[at + e] = list_tok[e] = 0x7fffffff;
+      p.vu[at + e] = list_vu[e] = -1;
     }
     start = next;
   }
-  __threadfence_block();
   __syncthreads();
   for (int t = tid / 32; t < p.chunk / W_TILE; t += PLAN_THREADS / 32) {
-    const int jt = p.tok[at + t * W_TILE + (tid & 31)], vt = p.vu[at + t * W_TILE + (tid & 31)];
-    TileSum x = {jt, jt, vt, vt};
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-      x.tmin = min(x.tmin, __shfl_xor(x.tmin, off, 64));
-      x.tmax = max(x.tmax, __shfl_xor(x.tmax, off, 64));
-      x.vmin = min(x.vmin, __shfl_xor(x.vmin, off, 64));
-      x.vmax = max(x.vmax, __shfl_xor(x.vmax, off, 64));
-    }
+    const int jt = list_tok[t * W_TILE + (tid & 31)], vt = list_vu[t * W_TILE + (tid & 31)];
+    const auto least = [](int a, int b) { return min(a, b); };
+    const auto most = [](int a, int b) { return max(a, b); };
+    const TileSum x = {half_wave_of(jt, least), half_wave_of(jt, most), half_wave_of(vt, least),
+                       half_wave_of(vt, most)};
     if ((tid & 31) == 0) p.sum[at / W_TILE + t] = x;
   }
 }
