@@ -920,7 +920,9 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
 //  * stats: a wave keeps two tiles of bf16 queries where that leaves W_UNITS
 //    waves (16 x 64 queries over 2048 rows of 64: 72 with one tile, 65 with two;
 //    32 heads of 2048 tokens: 74, 67), else one.  The rows are cut into
-//    up to 64 shares of at least 128 until there are W_FILL waves, two a SIMD.
+//    up to 64 shares of at least 128 (fp32, whose products take eight times as
+//    long: 64; 4 heads of 256 rows, 32 queries: 21.5 with 128, 17.6 with 64)
+//    until there are W_FILL waves, two a SIMD.
 //  * sums: up to 32 queries (bf16: 64) are kept by every wave, which streams
 //    rows (`votes`: W_FILL waves, up to 16 tiles each; 16 x 64 queries over 2048
 //    rows of 80: 66, with 4096 waves 69; 32 heads of 16000 rows 38, 41).
@@ -964,7 +966,8 @@ static WeightShape weight_shape(bool bf16, int64_t slices, int32_t nq, int32_t L
   if (nq > W_TILE && slices * ((nq + pair - 1) / pair) >= W_UNITS) w.keep = two;
   w.qtiles = (nq + w.keep * W_TILE - 1) / (w.keep * W_TILE);
   const int64_t units = slices * w.qtiles, want = (W_FILL + units - 1) / units;
-  w.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, 64, (L_cap + 127) / 128}));
+  const int share = bf16 ? 128 : 64;
+  w.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, 64, (L_cap + share - 1) / share}));
   return w;
 }
 
