@@ -510,7 +510,9 @@ int cached_attn_weights(const void* q, const void* k_cache, const float* w_in, f
  * to [0, L_cap], get w_in; nothing is written for the new row).
  * w_in, w_out : [b][H][L_cap] float; w_in nullable (zeros); w_out may be w_in.
  * ws       : >= sckv_decode_weights_workspace_bytes(b, H, L_cap, d_head).
- * Everything else as for compacted_decode_attn, whose outputs these are.
+ * Everything else as for compacted_decode_attn, whose outputs these are (the
+ * new row's rotation is computed in 64 bits here, so that a bf16 key may be
+ * stored one rounding step from that call's).
  * ------------------------------------------------------------------------- */
 size_t sckv_decode_weights_workspace_bytes(int32_t b, int32_t H, int32_t L_cap, int32_t d_head);
 int compacted_decode_attn_weights(const void* q, const void* k_new, const void* v_new,
@@ -574,7 +576,7 @@ int kv_compact_weights(float* w, float* w_out, int32_t M, int32_t b, int32_t H, 
  *            L_cap, d_head) bytes (overwritten; calls that share one must be
  *            ordered).
  * Everything else as for compacted_decode_attn, new row, <CL> steps, failures
- * and status included.
+ * and status included (the rotation as for compacted_decode_attn_weights).
  * ------------------------------------------------------------------------- */
 size_t sckv_shared_decode_workspace_bytes(int32_t b, int32_t H, int32_t n_prefix, int32_t P_cap,
                                           int32_t L_cap, int32_t d_head);
