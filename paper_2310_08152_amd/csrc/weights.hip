@@ -936,6 +936,8 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
 //    heads of 16384 tokens of 64: 1000, 1050 with one; 2 x 32 heads of 4096:
 //    213, 190), but of 64 elements only: of 80 their registers leave two waves
 //    a SIMD (16 x 4096 tokens: 1872, 1593).
+constexpr int W_SPLITS = 64;
+constexpr int W_MIN_SHARE = 64;
 constexpr int W_FILL = 2048;
 constexpr int W_UNITS = 512;
 constexpr int W_SHARE = 4096;
@@ -966,8 +968,8 @@ static WeightShape weight_shape(bool bf16, int64_t slices, int32_t nq, int32_t L
   if (nq > W_TILE && slices * ((nq + pair - 1) / pair) >= W_UNITS) w.keep = two;
   w.qtiles = (nq + w.keep * W_TILE - 1) / (w.keep * W_TILE);
   const int64_t units = slices * w.qtiles, want = (W_FILL + units - 1) / units;
-  const int share = bf16 ? 128 : 64;
-  w.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, 64, (L_cap + share - 1) / share}));
+  const int share = bf16 ? 2 * W_MIN_SHARE : W_MIN_SHARE;
+  w.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, W_SPLITS, (L_cap + share - 1) / share}));
   return w;
 }
 
@@ -1056,11 +1058,13 @@ using namespace sckv;
 extern "C" size_t sckv_attn_weights_workspace_bytes(int32_t b, int32_t H, int32_t nq,
                                                     int32_t L_cap) {
   if (b <= 0 || H <= 0 || nq < 0 || L_cap <= 0) return 0;
-  // (the size function is not told the element type)
-  const int64_t slices = (int64_t)b * H;
-  const int splits = std::max(weight_shape(true, slices, nq, L_cap).splits,
-                              weight_shape(false, slices, nq, L_cap).splits);
-  return plan_bytes(b, L_cap) + (size_t)slices * splits * nq * sizeof(float2);
+  // A bound that grows with nq, so that a workspace holds every smaller call
+  // too (fewer queries may be cut into more shares).  Shares are at most S and
+  // at most W_FILL / units + 1, of units of at most two tiles of queries.
+  const size_t rows = (size_t)b * H * nq;
+  const size_t S = std::min(W_SPLITS, (L_cap + W_MIN_SHARE - 1) / W_MIN_SHARE);
+  return plan_bytes(b, L_cap) +
+         (rows + std::min(rows * (S - 1), (size_t)W_FILL * 2 * W_TILE)) * sizeof(float2);
 }
 
 extern "C" int cached_attn_weights(const void* q, const void* k_cache, const float* w_in,

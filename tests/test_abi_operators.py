@@ -204,3 +204,14 @@ def test_no_kernel_spills(source, tmp_path):
     spilled = [int(x) for x in re.findall(r"VGPRs Spill: (\d+)", r.stderr)]
     assert names and len(names) == len(scratch) == len(spilled)
     assert not [n for n, s, v in zip(names, scratch, spilled) if s or v]
+
+
+@pytest.mark.parametrize("b,H,L_cap", [(1, 4, 256), (1, 32, 2000), (16, 32, 4096), (3, 7, 65536)])
+def test_weights_workspace_serves_fewer_queries(B, b, H, L_cap):
+    """A workspace for the most queries of a call holds every smaller call (a
+    prompt's ragged last block)."""
+    most = 0
+    for nq in [*range(1, 300), 511, 512, 513, 1023, 1024, 1025, 2047, 2049, 4096, 65535, 65536]:
+        n = B.sckv_attn_weights_workspace_bytes(b, H, nq, L_cap)
+        assert n >= most, (nq, n, most)
+        most = n

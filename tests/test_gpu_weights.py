@@ -395,3 +395,16 @@ def test_decode_weights_in_a_graph(b, H, cap):
         outs.append((o, cache.w.clone(), cache.kv_len.clone()))
     for a, c in zip(*outs):
         assert torch.equal(a, c)
+
+
+def test_workspace_of_more_queries():
+    """Calls of fewer queries than the workspace was made for."""
+    print("weights workspace", flush=True)
+    b, H, d, L = 1, 4, 64, 3000
+    spans = [R.some_spans(L, 3)]
+    h = Held(b, H, L, d, torch.bfloat16, L, spans, [list(range(L))], 8, 33)
+    for n in (33, 32, 5, 1):
+        out = torch.zeros(b, H, L, device=DEV)
+        h.q = h.q[:, :, -n:]
+        P().prompt_weights(h.q, h.cache, 0, h.meta, h.ws, L - n, None, out)
+        h.check(out, torch.zeros_like(out), L - n)
