@@ -189,13 +189,13 @@ __device__ __forceinline__ void keep_weights(const StepWeights& x, int64_t at, i
 // slice's maximum M (log2 units) and sum of weights L
 __device__ __forceinline__ void add_weights(const StepWeights& x, int64_t at, int n, int r0, int r1,
                                             float M, float L, int tid, int nthr,
-                                            const OldSums* first = nullptr) {
+                                            const OldSums& first) {
   const float inv = 1.f / L;
   for (int base = r0 + tid; base < r1; base += OLD_SUMS * nthr) {
     OldSums old;
     float sc[OLD_SUMS];
-    if (first && base == r0 + tid) {
-      old = *first;
+    if (base == r0 + tid) {
+      old = first;
     } else {
       old.load(x, at, n, base, nthr);
     }
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(THREADS) void decode_chunk_kernel(
     }
     if constexpr (FINAL && X::PREFIX) pre.join(x, bh, tid, M, Lsum, ov);
     if constexpr (FINAL && X::WEIGHTS)
-      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, M, Lsum, tid, THREADS, &old);
+      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, M, Lsum, tid, THREADS, old);
     if (tid >= D) {
     } else if constexpr (FINAL) {
       res[tid] = ov / Lsum;
@@ -531,6 +531,20 @@ __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
   }
   const int t = cur_tok[s];
   const int n = ring > 0 ? ring : kv_len[s];  // the ring is always full
+  // rows of a workgroup that adds weights: asked for before the step's kind and
+  // the slice's maximum and sum are known (a row past the last is read as it)
+  const int64_t wat = (int64_t)bh * L_cap;
+  const int r0 = (blk - 1) * WEIGHT_ROWS, r_end = min(max(n, 0), L_cap - 1);
+  OldSums old;
+  float sc[OLD_SUMS];
+  if constexpr (X::WEIGHTS) {
+    static_assert(WEIGHT_ROWS == OLD_SUMS * 64 * COMBINE_WAVES, "one batch of rows");
+    if (blk > 0 && r0 <= r_end) {
+      old.load(x, wat, r_end, r0 + tid, 64 * COMBINE_WAVES);
+#pragma unroll
+      for (int i = 0; i < OLD_SUMS; ++i) sc[i] = x.scores[wat + min(r0 + tid + i * 64 * COMBINE_WAVES, r_end)];
+    }
+  }
   // the step kind, as step_kind()
   const int kind = (t < 0 || t >= L_meta)                       ? 2
                    : vu[(int64_t)s * L_meta + t] == t           ? 1
@@ -539,13 +553,12 @@ __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
   if (kind != 0) {
     if (blk == 0) write_special<T, D>(kind, v_new, o, status, bh, H, tid, 64 * COMBINE_WAVES);
     if constexpr (X::WEIGHTS)
-      if (blk == 1) keep_weights(x, (int64_t)bh * L_cap, min(max(n, 0), L_cap), tid, 64 * COMBINE_WAVES);
+      if (blk == 1) keep_weights(x, wat, min(max(n, 0), L_cap), tid, 64 * COMBINE_WAVES);
     return;
   }
   const int nch = chunk_plan(n + 1, sp).n;
   if constexpr (X::WEIGHTS) {
     if (blk > 0) {
-      const int r0 = (blk - 1) * WEIGHT_ROWS;
       if (r0 > n) return;
       float Mw = -INFINITY, lw = 0.f;
       for (int c0 = 0; c0 < nch; c0 += 64) {
@@ -556,8 +569,12 @@ __global__ __launch_bounds__(64 * COMBINE_WAVES) void decode_combine_kernel(
         lw = lw * exp2f(Mw - mn) + wave_sum(lc * exp2f(mc - mn));
         Mw = mn;
       }
-      add_weights(x, (int64_t)bh * L_cap, n, r0, min(r0 + WEIGHT_ROWS, n + 1), Mw, lw, tid,
-                  64 * COMBINE_WAVES);
+      const float inv = 1.f / lw;
+#pragma unroll
+      for (int i = 0; i < OLD_SUMS; ++i) {
+        const int row = r0 + tid + i * 64 * COMBINE_WAVES;
+        if (row <= n) x.w_out[wat + row] = fmaf(fast_exp2(sc[i] - Mw), inv, old.v[i]);
+      }
       return;
     }
   }
@@ -936,7 +953,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     }
     if constexpr (FINAL && X::PREFIX) pre.join(x, bh, tid, Mx, Ls, ov);
     if constexpr (FINAL && X::WEIGHTS)
-      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, Mx, Ls, tid, THREADS, &old);
+      add_weights(x, (int64_t)bh * L_cap, n, 0, rows, Mx, Ls, tid, THREADS, old);
     if (tid >= D) {
     } else if constexpr (FINAL) {
       o[(int64_t)bh * D + tid] = f32_to_bf16(ov / Ls);
