@@ -578,14 +578,11 @@ struct Stage {
   }
 };
 
-// Waves of a SIMD that the registers are held to: four where one register less
-// gives them (d = 64; 2 x 32 heads of 4096 tokens 222 -> 190 us), else what the
-// compiler leaves.
-constexpr int staged_waves(bool bf16, int D, bool fits) { return bf16 && D == 64 && fits ? 4 : 2; }
-
-// stats of large launches: QT tiles of queries a wave, W_WAVES * QT a workgroup
+// stats of large launches: QT tiles of queries a wave, W_WAVES * QT a workgroup;
+// four waves a SIMD where three registers less give them (d = 64; 2 x 32 heads of
+// 4096 tokens 222 -> 213 us)
 template <typename T, int D, int QT>
-__global__ __launch_bounds__(64 * W_WAVES, staged_waves(sizeof(T) == 2, D, true)) void weight_stats_staged_kernel(
+__global__ __launch_bounds__(64 * W_WAVES, sizeof(T) == 2 && D == 64 ? 4 : 2) void weight_stats_staged_kernel(
     const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, float2* __restrict__ ml,
     int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c, const int32_t* __restrict__ vu,
     int32_t L_meta, int32_t tok0, int32_t n_slice, int32_t qgroups, int32_t splits) {
@@ -705,15 +702,18 @@ __global__ __launch_bounds__(64 * W_WAVES, staged_waves(sizeof(T) == 2, D, true)
   }
 }
 
-// sums of large launches: KT tiles of rows a wave, W_WAVES * KT a workgroup
+// sums of large launches: KT tiles of rows a wave, W_WAVES * KT a workgroup.
+// The tiles are S = Q K^T here: the lane owns row l % 32 and its token, vu and
+// sum, in five registers a tile of rows instead of 16 (16 x 4096 tokens of 80:
+// 1586 -> 1486 us; 2 x 32 heads of 64: 187 -> 178).
 template <typename T, int D, int KT>
-__global__ __launch_bounds__(64 * W_WAVES, staged_waves(sizeof(T) == 2, D, KT == 1)) void weight_sums_staged_kernel(
+__global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
     const T* __restrict__ q, const T* __restrict__ k, WeightPlan p, const float2* __restrict__ ml,
     const float* w_in, float* w_out, int32_t H, int32_t nq, int64_t q_s, int64_t k_s, float c,
     int32_t tok0, int32_t L_cap, int32_t n_slice, int32_t splits) {
   using S = Stage<T, D>;
   __shared__ __align__(16) char lds[2][S::BYTES];
-  __shared__ float lse[2][S::ROWS];
+  __shared__ __align__(16) float lse[2][S::ROWS];
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wg = blockIdx.x / n_slice, slice = blockIdx.x - wg * n_slice;
@@ -742,15 +742,19 @@ __global__ __launch_bounds__(64 * W_WAVES, staged_waves(sizeof(T) == 2, D, KT ==
   const int t0 = g0 + wave * KT;
   TileSum ts[KT];
   Operand<T, D> K[KT];
-  f32x16 acc[KT];
+  // the lane's row of each tile: list entry, token, vu, sum
+  int e[KT], tok[KT], vus[KT];
+  float acc[KT][2];
 #pragma unroll
   for (int x = 0; x < KT; ++x) {
     const bool in = t0 + x < n_tiles;
     ts[x] = in ? sums[t0 + x] : TileSum{0x7fffffff, 0x7fffffff, -1, -1};
-    const int e = in ? p.row[at + (int64_t)(t0 + x) * W_TILE + l32] : -1;
-    K[x].load(kb + (int64_t)(max(e, 0) & (W_CL - 1)) * D, h);
-#pragma unroll
-    for (int v = 0; v < 16; ++v) acc[x][v] = 0.f;
+    const int64_t i = at + (int64_t)(t0 + x) * W_TILE + l32;
+    e[x] = in ? p.row[i] : -1;
+    tok[x] = in ? p.tok[i] : 0;
+    vus[x] = in ? p.vu[i] : -1;
+    K[x].load(kb + (int64_t)(max(e[x], 0) & (W_CL - 1)) * D, h);
+    acc[x][0] = acc[x][1] = 0.f;
   }
   const float2* mls = ml + (int64_t)slice * splits * nq;
   S st;
@@ -787,33 +791,37 @@ __global__ __launch_bounds__(64 * W_WAVES, staged_waves(sizeof(T) == 2, D, KT ==
       const int ta = tok0 + g * S::ROWS + y * W_TILE, tb = min(ta + W_TILE - 1, last);
       if (ta > last) continue;
       S::read(Q, lds[buf], y, lane);
-      const float ls = lse[buf][y * W_TILE + l32];
+      float4 ls[4];  // of the lane's queries, as the registers of a score tile
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ls[i] = *reinterpret_cast<const float4*>(&lse[buf][y * W_TILE + 8 * i + 4 * h]);
 #pragma unroll
       for (int x = 0; x < KT; ++x) {
         if (ts[x].tmin > tb || ts[x].vmax < ta) continue;
-        f32x16 sc = scores<T, D>(K[x], Q);
+        f32x16 sc = scores<T, D>(Q, K[x]);  // S = Q K^T: the lane owns a row
         if (ts[x].tmax > ta || ts[x].vmin < tb) {
-          const int64_t e = at + (int64_t)(t0 + x) * W_TILE;
-          mask_scores(sc, p.tok + e, p.vu + e, ta + l32, h);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int tq = ta + 8 * (v / 4) + 4 * h + v % 4;
+            sc[v] = tok[x] <= tq && tq <= vus[x] ? sc[v] : -INFINITY;
+          }
         }
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[x][v] += fast_exp2(fmaf(sc[v], c, -ls));
+        for (int i = 0; i < 4; ++i) {
+          acc[x][0] += fast_exp2(fmaf(sc[4 * i], c, -ls[i].x));
+          acc[x][1] += fast_exp2(fmaf(sc[4 * i + 1], c, -ls[i].y));
+          acc[x][0] += fast_exp2(fmaf(sc[4 * i + 2], c, -ls[i].z));
+          acc[x][1] += fast_exp2(fmaf(sc[4 * i + 3], c, -ls[i].w));
+        }
       }
     }
     buf ^= 1;
   }
 #pragma unroll
   for (int x = 0; x < KT; ++x) {
-    float v[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = acc[x][i];
-    int base = 0;
-    half_wave_reduce<16, 16>(v, lane, base);
-    const int m = 8 * (base / 4) + 4 * h + base % 4;
-    const int e = t0 + x < n_tiles && !(lane & 1) ? p.row[at + (int64_t)(t0 + x) * W_TILE + m] : -1;
-    if (e < 0) continue;
-    const int64_t r = (int64_t)slice * L_cap + (e & (W_CL - 1));
-    w_out[r] = (w_in ? w_in[r] : 0.f) + (e & W_CL ? 1.f : v[0]);
+    const float total = other_half(acc[x][0] + acc[x][1], true);
+    if (h || e[x] < 0) continue;
+    const int64_t r = (int64_t)slice * L_cap + (e[x] & (W_CL - 1));
+    w_out[r] = (w_in ? w_in[r] : 0.f) + (e[x] & W_CL ? 1.f : total);
   }
 }
 
@@ -933,9 +941,8 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_votes_kernel(
 //    staged in LDS.  A wave keeps two tiles of queries where 2 W_WGS workgroups
 //    do (32 heads of 8192 tokens of 80: 558 with two, 587 with one), else one
 //    (4096 tokens: 198, 179).  Two tiles of rows where 4 W_WGS workgroups do (32
-//    heads of 16384 tokens of 64: 1000, 1050 with one; 2 x 32 heads of 4096:
-//    213, 190), but of 64 elements only: of 80 their registers leave two waves
-//    a SIMD (16 x 4096 tokens: 1872, 1593).
+//    heads of 16384 tokens of 64: 954, 971 with one; 16 x 32 of 4096 of 80: 1486,
+//    1520; 2 x 32 of 4096 of 64: 204, 180).
 constexpr int W_SPLITS = 64;
 constexpr int W_MIN_SHARE = 64;
 constexpr int W_FILL = 2048;
@@ -1032,11 +1039,10 @@ static int launch_weights(const void* q, const void* k, const float* w_in, float
     if (sh.votes == NT) vote(weight_votes_kernel<T, D, NT>);
     else vote(weight_votes_kernel<T, D, 1>);
   } else if (sh.staged) {
-    constexpr int KT = D == 64 ? NT : 1;
-    const int kt = slices * (tiles / (W_WAVES * KT)) >= 4 * W_WGS ? KT : 1;
+    const int kt = slices * (tiles / (W_WAVES * NT)) >= 4 * W_WGS ? NT : 1;
     rc = grid((tiles + W_WAVES * kt - 1) / (W_WAVES * kt));
     if (rc) return rc;
-    if (kt == KT) go(weight_sums_staged_kernel<T, D, KT>);
+    if (kt == NT) go(weight_sums_staged_kernel<T, D, NT>);
     else go(weight_sums_staged_kernel<T, D, 1>);
   } else {
     const int kt = slices * (tiles / NT) >= W_FILL ? NT : 1;
