@@ -704,7 +704,7 @@ __global__ __launch_bounds__(64 * W_WAVES, sizeof(T) == 2 && D == 64 ? 4 : 2) vo
 
 // sums of large launches: KT tiles of rows a wave, W_WAVES * KT a workgroup.
 // The tiles are S = Q K^T here: the lane owns row l % 32 and its token, vu and
-// sum, in five registers a tile of rows instead of 16 (16 x 4096 tokens of 80:
+// sum, in four registers a tile of rows instead of 16 (16 x 4096 tokens of 80:
 // 1586 -> 1486 us; 2 x 32 heads of 64: 187 -> 178).
 template <typename T, int D, int KT>
 __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
@@ -744,7 +744,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
   Operand<T, D> K[KT];
   // the lane's row of each tile: list entry, token, vu, sum
   int e[KT], tok[KT], vus[KT];
-  float acc[KT][2];
+  float acc[KT];
 #pragma unroll
   for (int x = 0; x < KT; ++x) {
     const bool in = t0 + x < n_tiles;
@@ -754,7 +754,7 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
     tok[x] = in ? p.tok[i] : 0;
     vus[x] = in ? p.vu[i] : -1;
     K[x].load(kb + (int64_t)(max(e[x], 0) & (W_CL - 1)) * D, h);
-    acc[x][0] = acc[x][1] = 0.f;
+    acc[x] = 0.f;
   }
   const float2* mls = ml + (int64_t)slice * splits * nq;
   S st;
@@ -805,20 +805,23 @@ __global__ __launch_bounds__(64 * W_WAVES, 2) void weight_sums_staged_kernel(
             sc[v] = tok[x] <= tq && tq <= vus[x] ? sc[v] : -INFINITY;
           }
         }
+        // (a tile's sum first: the rounding of a long sum grows with its terms)
+        float a0 = 0.f, a1 = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          acc[x][0] += fast_exp2(fmaf(sc[4 * i], c, -ls[i].x));
-          acc[x][1] += fast_exp2(fmaf(sc[4 * i + 1], c, -ls[i].y));
-          acc[x][0] += fast_exp2(fmaf(sc[4 * i + 2], c, -ls[i].z));
-          acc[x][1] += fast_exp2(fmaf(sc[4 * i + 3], c, -ls[i].w));
+          a0 += fast_exp2(fmaf(sc[4 * i], c, -ls[i].x));
+          a1 += fast_exp2(fmaf(sc[4 * i + 1], c, -ls[i].y));
+          a0 += fast_exp2(fmaf(sc[4 * i + 2], c, -ls[i].z));
+          a1 += fast_exp2(fmaf(sc[4 * i + 3], c, -ls[i].w));
         }
+        acc[x] += a0 + a1;
       }
     }
     buf ^= 1;
   }
 #pragma unroll
   for (int x = 0; x < KT; ++x) {
-    const float total = other_half(acc[x][0] + acc[x][1], true);
+    const float total = other_half(acc[x], true);
     if (h || e[x] < 0) continue;
     const int64_t r = (int64_t)slice * L_cap + (e[x] & (W_CL - 1));
     w_out[r] = (w_in ? w_in[r] : 0.f) + (e[x] & W_CL ? 1.f : total);
