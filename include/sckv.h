@@ -511,8 +511,8 @@ int cached_attn_weights(const void* q, const void* k_cache, const float* w_in, f
  * w_in, w_out : [b][H][L_cap] float; w_in nullable (zeros); w_out may be w_in.
  * ws       : >= sckv_decode_weights_workspace_bytes(b, H, L_cap, d_head).
  * Everything else as for compacted_decode_attn, whose outputs these are (the
- * new row's rotation is computed in 64 bits here, so that a bf16 key may be
- * stored one rounding step from that call's).
+ * new row of a bf16 cache is turned by sines and cosines of 64 bits here, so
+ * that its key may be stored one rounding step from that call's).
  * ------------------------------------------------------------------------- */
 size_t sckv_decode_weights_workspace_bytes(int32_t b, int32_t H, int32_t L_cap, int32_t d_head);
 int compacted_decode_attn_weights(const void* q, const void* k_new, const void* v_new,

@@ -133,9 +133,17 @@ __device__ __forceinline__ void load_rotated_piece(const T* x, int seg, bool rot
   }
 }
 
+// two products and their sum, each rounded (never fused)
+__device__ __forceinline__ float plain_turn(float x, float y, float cs, float sn) {
+#pragma clang fp contract(off)
+  const float a = x * cs;
+  const float b = y * sn;
+  return a + b;
+}
+
 // What a launch does beside the step itself.
 struct StepOnly {
-  static constexpr bool WEIGHTS = false, PREFIX = false, EXACT_ROTATION = false;
+  static constexpr bool WEIGHTS = false, PREFIX = false, PLAIN_ROTATION = false;
 };
 // Adds the step's softmax weights to each row's accumulated weight.  A row's
 // weight needs the whole slice's maximum and sum, so the scores (log2 units)
@@ -144,7 +152,7 @@ struct StepOnly {
 // kept in LDS where one workgroup has the slice and the cache's capacity fits
 // (`in_lds`), else in `scores`; computing them again would read the keys twice.
 struct StepWeights {
-  static constexpr bool WEIGHTS = true, PREFIX = false, EXACT_ROTATION = true;
+  static constexpr bool WEIGHTS = true, PREFIX = false, PLAIN_ROTATION = true;
   const float* w_in;
   float* w_out;
   float* scores;  // [slice][L_cap]
@@ -173,7 +181,7 @@ struct OldSums {
 };
 // Joins the partials of a shared prefix (one per chunk of it) to the slice's.
 struct StepPrefix {
-  static constexpr bool WEIGHTS = false, PREFIX = true, EXACT_ROTATION = true;
+  static constexpr bool WEIGHTS = false, PREFIX = true, PLAIN_ROTATION = true;
   const float* o;    // [slice][n][d], unnormalised
   const float2* ml;  // [slice][n]: maximum (log2 units), sum of weights
   int32_t n;
@@ -777,18 +785,19 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
   if (tid < D) {
     float x = bf16_lo((uint32_t)qx_raw);
     float kx = bf16_lo((uint32_t)kx_raw);
-    if (X::EXACT_ROTATION && rotate) {
-      // in 64 bits, so that the stored key is the exact one's rounding: a key
-      // element rounded to its other neighbour moves the fp32 weights by more
-      // than all their own rounding
-      const double pv = bf16_lo((uint32_t)qp_raw), kp = bf16_lo((uint32_t)kp_raw);
+    if (X::PLAIN_ROTATION && rotate) {
+      // sine and cosine in 64 bits, each rounded once, then two products and a
+      // sum rounded to fp32: the stored key is that of plain fp32 arithmetic,
+      // bit for bit.  (A key element rounded to its other bf16 neighbour moves
+      // the fp32 weights by more than all their own rounding.)
+      const float pv = bf16_lo((uint32_t)qp_raw), kp = bf16_lo((uint32_t)kp_raw);
       double turns = (double)pos_t * freq * 0.15915494309189533576888376337251;
       turns -= rint(turns);
-      double sn, cs;
-      sincospi(2.0 * turns, &sn, &cs);
-      if (tid < HD) sn = -sn;
-      x = (float)((double)x * cs + pv * sn);
-      kx = (float)((double)kx * cs + kp * sn);
+      double sd, cd;
+      sincospi(2.0 * turns, &sd, &cd);
+      const float cs = (float)cd, sn = (float)(tid < HD ? -sd : sd);
+      x = plain_turn(x, pv, cs, sn);
+      kx = plain_turn(kx, kp, cs, sn);
     } else if (rotate) {
       const float pv = bf16_lo((uint32_t)qp_raw);
       const float kp = bf16_lo((uint32_t)kp_raw);

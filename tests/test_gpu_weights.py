@@ -408,3 +408,24 @@ def test_workspace_of_more_queries():
         h.q = h.q[:, :, -n:]
         P().prompt_weights(h.q, h.cache, 0, h.meta, h.ws, L - n, None, out)
         h.check(out, torch.zeros_like(out), L - n)
+
+
+@pytest.mark.parametrize("d", (64, 80))
+def test_stored_key_is_plain_arithmetic(d):
+    """The new bf16 key: sine and cosine in 64 bits, rounded once; products and
+    sum in fp32, each rounded; the same bits, at far positions too."""
+    print("weights key", d, flush=True)
+    b, H, T = 9, 32, 9000
+    toks = [0, 1, 7, 100, 1023, 2048, 5000, 8191, 8999]
+    h = Held(b, H, 64, d, torch.bfloat16, T, [[] for _ in range(b)], [[0]] * b, 3, 1)
+    c = h.cache
+    c.cur_tok.copy_(torch.tensor(toks))
+    q, k, v = (R.rand((b, H, d), 5 + i, torch.bfloat16, 1.0, DEV) for i in range(3))
+    o = torch.empty_like(q)
+    P().decode_weights_layer(q, k, v, c, 0, h.meta, h.ws, o, theta=1e4)
+    a = torch.tensor(toks, dtype=torch.float64)[:, None, None] * \
+        1e4 ** (-torch.arange(d // 2, dtype=torch.float64) / (d // 2))
+    cs, sn, x = a.cos().float(), a.sin().float(), k.cpu().float()
+    x1, x2 = x[..., :d // 2], x[..., d // 2:]
+    want = torch.cat([x1 * cs - x2 * sn, x2 * cs + x1 * sn], -1).bfloat16()
+    assert torch.equal(c.k(0)[:, :, 1].cpu(), want)
